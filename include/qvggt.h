@@ -22,8 +22,8 @@
  *     owns every buffer except the opaque weights handle.
  *   - bf16 buffers are passed as void*; packed int4 buffers as unsigned char*: byte i of a row holds
  *     code 2i in bits 0-3 and code 2i+1 in bits 4-7, two's complement.
- *   - K must be 1024 or 4096 (the rotation is a power-of-two Hadamard; other sizes: QVGGT_ERR_SHAPE).
- *     N must be a multiple of 128.  M >= 0 (M == 0 is a no-op).
+ *   - K must be 1024 or 4096 (the rotation is a power-of-two Hadamard; other sizes: QVGGT_ERR_SHAPE) and N a
+ *     multiple of 128, except on the rotation-free 8-bit path (qvggt_quantize_c8 and what follows it).  M >= 0 (M == 0 is a no-op).
  *   - `group` selects the activation-scale granularity: 0 = one scale per token (the paper's
  *     setting); 128 = one scale per token per 128 consecutive rotated channels (an extension; the
  *     integer partial sums are rescaled per group in the epilogue).
@@ -265,6 +265,61 @@ int qvggt_debug_starved_linear_c8(const qvggt_weights_t *w, const signed char *X
 int qvggt_gelu_rotate_smooth_quantize_c8(const qvggt_weights_t *w, const void *X_bf16, long long ldx, int M,
                                          signed char *Xq8, float *a_scale, void *cuda_stream);
 int qvggt_gelu(const void *X_bf16, long long ldx, int M, int K, void *Y_bf16, void *cuda_stream);
+
+/*
+ * The rotation-free 8-bit path: the paper's "naive" W8A8 arm (Tab. "efficiency", 8/8 naive) and any layer whose codes do not come
+ * from a rotated handle -- RMS norms, other widths, weights quantized elsewhere.  Rows of any length K from 1 to 131056, rows of any
+ * leading dimension from K on; activations, residual, results and bias are of one of three types; all arithmetic is fp32.
+ *
+ * Per row:  amax = max(max_k |y[k]|, 1e-8),  scale = amax / 127,  q[k] = round(y[k] * (127 * (1 / amax))), codes in [-127, 127]
+ * (every operation rounded to fp32 by itself, then half to even).
+ * A row that holds a NaN or an infinity gets the scale NaN and codes 0, so that every result computed from it is NaN.
+ */
+#define QVGGT_BF16 0
+#define QVGGT_FP16 1
+#define QVGGT_FP32 2
+
+/*
+ * Rows to 8-bit codes and scales: activations without a norm in front of them, or weights (one scale per output channel).
+ *   X        [M, K] of `type`, row stride ldx elements, aligned to its elements
+ *   Xq8      int8 [M, K], row stride ldq bytes (qvggt_linear_c8 wants a multiple of 16); bytes between rows are left as they were
+ *   a_scale  fp32 [M]
+ */
+int qvggt_quantize_c8(const void *X, int type, long long ldx, int M, int K, signed char *Xq8, long long ldq, float *a_scale,
+                      void *cuda_stream);
+
+/* The values that codes stand for: Y[m][k] = Xq8[m][k] * a_scale[m], rounded to `type`. */
+int qvggt_dequantize_c8(const signed char *Xq8, long long ldq, const float *a_scale, int M, int K, void *Y, int type, long long ldy,
+                        void *cuda_stream);
+
+/*
+ * RMS norm with the residual's addition:
+ *   h[k] = X[k] + residual[k] (X[k] without residual),  Y[k] = (h[k] * rstd) * gamma[k],  rstd = 1 / sqrt(sum(h * h) / K + eps)
+ * The sum is kept in fp32 for the norm; H, if given, receives it rounded to the type.  The squares are summed in fp32: rows whose
+ * sum of squares is beyond its range give 0 (NaN where an element is infinite).
+ *   residual  [M, K] or NULL;  H [M, K] or NULL;  gamma fp32 [K];  eps >= 0, finite
+ * H and Y may each be X or residual itself (the same pointer and stride), not overlap them, or one another, in any other way.
+ */
+int qvggt_rmsnorm(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K, const float *gamma,
+                  float eps, void *H, long long ldh, void *Y, long long ldy, void *cuda_stream);
+
+/* The same norm with its output in 8 bits: the unrounded y goes straight into the quantizer and never to memory. */
+int qvggt_rmsnorm_quantize_c8(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K,
+                              const float *gamma, float eps, void *H, long long ldh, signed char *Xq8, long long ldq, float *a_scale,
+                              void *cuda_stream);
+
+/*
+ * Product of 8-bit codes with scales for each token and channel:
+ *   Y[m][n] = float(acc) * (a_scale[m] * w_scale[n]) + bias[n],  acc = sum_k Xq8[m][k] * Wq8[n][k] exactly, in int32
+ * (the product of the scales is rounded, then the multiply-add once, then to the type).  A row's results do not depend on M.
+ *   Xq8   int8 [M, K], row stride ldx;  Wq8  int8 [N, K], row stride ldw: 16-byte aligned, strides multiples of 16.  Codes may be
+ *         any int8.  What lies behind K in the 16 bytes that K ends in is read, and has no effect.
+ *   a_scale fp32 [M];  w_scale fp32 [N];  bias [N] of `type` or NULL
+ *   Y     [M, N] of `type`, row stride ldy elements, aligned to its elements.  Rows are written fastest where they begin on 16-byte
+ *         boundaries.  What lies between the rows is left as it was.
+ */
+int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw,
+                    const float *w_scale, const void *bias, int M, int N, int K, void *Y, int type, long long ldy, void *cuda_stream);
 
 /* Frees the handle and its device memory (synchronises the device first).  At most 64 MB per device stay with the library for
  * the next handle; they go back to the driver when an allocation of the library fails.  NULL is allowed. */

@@ -30,7 +30,9 @@ EXPORTS = ("qvggt_prepare_weights", "qvggt_rotate_smooth_quantize", "qvggt_w4a4_
            "qvggt_rotate_smooth_quantize_tc", "qvggt_rotate_smooth_quantize_tc_c8", "qvggt_gelu",
            "qvggt_gelu_rotate_smooth_quantize_c8", "qvggt_w4a4_linear_c8_packed_weights",
            "qvggt_rotate_smooth_quantize_c8_grouped", "qvggt_w4a4_linear_c8_grouped",
-           "qvggt_rotate_smooth_quantize_c8_expand", "qvggt_w4a4_linear_c8_expanded")
+           "qvggt_rotate_smooth_quantize_c8_expand", "qvggt_w4a4_linear_c8_expanded",
+           "qvggt_quantize_c8", "qvggt_dequantize_c8", "qvggt_rmsnorm", "qvggt_rmsnorm_quantize_c8", "qvggt_linear_c8")
+TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # QVGGT_BF16, QVGGT_FP16, QVGGT_FP32
 PREP_C8 = 1   # QVGGT_PREP_C8: keep an int8 [N, K] copy of the weight codes for the *_c8 entry points
 PREP_W8A8 = 2  # QVGGT_PREP_W8A8: 8-bit codes (one per byte only)
 PREP_C8_ONLY = 4  # QVGGT_PREP_C8_ONLY: 4-bit codes one per byte only (no packed copy)
@@ -84,6 +86,11 @@ def lib() -> ctypes.CDLL:
         L.qvggt_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
         L.qvggt_calibrate_smooth.argtypes = [vp, i32, vp, i32, i32, f32, f32, f32, vp, vp, vp]
         L.qvggt_quantize_weights_static.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.qvggt_quantize_c8.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+        L.qvggt_dequantize_c8.argtypes = [vp, i64, vp, i32, i32, vp, i32, i64, vp]
+        L.qvggt_rmsnorm.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp]
+        L.qvggt_rmsnorm_quantize_c8.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp, vp]
+        L.qvggt_linear_c8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
         L.qvggt_status_string.argtypes = [i32]
         L.qvggt_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -502,3 +509,127 @@ def quantize_weights_static(W: torch.Tensor, smooth_c: torch.Tensor, sign_v: tor
     assert w_scale.dtype == torch.float32 and w_scale.numel() == N and amul.dtype == torch.float32 and amul.numel() == K
     _check(lib().qvggt_quantize_weights_static(_ptr(W), _ptr(smooth_c), _ptr(sign_v), N, K, _ptr(Wq), _ptr(w_scale),
                                                _ptr(amul), _stream()), "qvggt_quantize_weights_static")
+
+
+# ---------------------------------------------------------------- the rotation-free 8-bit path
+
+def _rows(t: torch.Tensor, M: int, K: int, dtype: torch.dtype) -> int:
+    """Checks a matrix of rows (unit stride along a row) and gives its row stride."""
+    assert t.dtype == dtype and t.shape == (M, K) and (K == 1 or t.stride(1) == 1)
+    assert t.is_cuda and t.device.index == torch.cuda.current_device(), "tensor of the current device expected"
+    return t.stride(0) if M > 1 else (K + 15) // 16 * 16
+
+
+def _vector(t: torch.Tensor, n: int, dtype: torch.dtype = torch.float32) -> int:
+    assert t.dtype == dtype and t.shape == (n,) and t.is_contiguous()
+    assert t.is_cuda and t.device.index == torch.cuda.current_device(), "tensor of the current device expected"
+    return t.data_ptr()
+
+
+def _new_codes(M: int, K: int, device) -> torch.Tensor:
+    """Codes as linear_c8 reads them: rows a multiple of 16 bytes apart."""
+    return torch.empty((M, (K + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :K]
+
+
+def quantize_c8(X: torch.Tensor, Xq8: torch.Tensor | None = None, a_scale: torch.Tensor | None = None):
+    """Rows to 8-bit codes, one scale per row, no rotation: X [M,K] bf16 / fp16 / fp32, any K and row stride -> (Xq8 [M,K] int8, a_scale
+    fp32 [M]).  New codes have rows a multiple of 16 bytes apart (a view, where K is no such multiple), as linear_c8 wants them."""
+    if _fast is not None:
+        r = _fast.quantize_c8(X, Xq8, a_scale)
+        if r is not None:
+            return r
+    assert X.dim() == 2 and X.dtype in TYPES
+    M, K = X.shape
+    ldx = _rows(X, M, K, X.dtype)
+    if Xq8 is None:
+        Xq8 = _new_codes(M, K, X.device)
+    if a_scale is None:
+        a_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+    _check(lib().qvggt_quantize_c8(_ptr(X), TYPES[X.dtype], ldx, M, K, _ptr(Xq8), _rows(Xq8, M, K, torch.int8), _vector(a_scale, M), _stream()),
+           "qvggt_quantize_c8")
+    return Xq8, a_scale
+
+
+def dequantize_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, dtype: torch.dtype = torch.bfloat16, Y: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that codes stand for: Xq8 [M,K] int8, a_scale fp32 [M] -> Y [M,K] of `dtype` (or of Y's own, where Y is given)."""
+    if _fast is not None and dtype in TYPES:
+        r = _fast.dequantize_c8(Xq8, a_scale, TYPES[dtype], Y)
+        if r is not None:
+            return r
+    assert Xq8.dim() == 2
+    M, K = Xq8.shape
+    ldq = _rows(Xq8, M, K, torch.int8)
+    if Y is None:
+        assert dtype in TYPES
+        Y = torch.empty((M, K), dtype=dtype, device=Xq8.device)
+    assert Y.dtype in TYPES
+    _check(lib().qvggt_dequantize_c8(_ptr(Xq8), ldq, _vector(a_scale, M), M, K, _ptr(Y), TYPES[Y.dtype], _rows(Y, M, K, Y.dtype), _stream()),
+           "qvggt_dequantize_c8")
+    return Y
+
+
+def _norm_arguments(X, gamma, residual, H):
+    assert X.dim() == 2 and X.dtype in TYPES
+    M, K = X.shape
+    ldx, g = _rows(X, M, K, X.dtype), _vector(gamma, K)
+    ldr = 0 if residual is None else _rows(residual, M, K, X.dtype)
+    if H is None and residual is not None:
+        H = torch.empty((M, K), dtype=X.dtype, device=X.device)
+    return M, K, ldx, ldr, g, H, 0 if H is None else _rows(H, M, K, X.dtype)
+
+
+def rmsnorm(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None, Y: torch.Tensor | None = None,
+            H: torch.Tensor | None = None):
+    """Y = h / sqrt(mean(h^2) + eps) * gamma with h = X (+ residual): X, residual [M,K] bf16 / fp16 / fp32, gamma fp32 [K] -> Y [M,K] of the
+    same type, or (Y, H) with H = h rounded to that type where there is a residual or H is given.  Y and H may be X or residual itself."""
+    if _fast is not None:
+        r = _fast.rmsnorm(X, gamma, eps, residual, Y, H)
+        if r is not None:
+            return r
+    M, K, ldx, ldr, g, H, ldh = _norm_arguments(X, gamma, residual, H)
+    if Y is None:
+        Y = torch.empty((M, K), dtype=X.dtype, device=X.device)
+    _check(lib().qvggt_rmsnorm(_ptr(X), _ptr(residual), TYPES[X.dtype], ldx, ldr, M, K, g, eps, _ptr(H), ldh, _ptr(Y), _rows(Y, M, K, X.dtype),
+                               _stream()), "qvggt_rmsnorm")
+    return Y if H is None else (Y, H)
+
+
+def rmsnorm_quantize_c8(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
+                        Xq8: torch.Tensor | None = None, a_scale: torch.Tensor | None = None, H: torch.Tensor | None = None):
+    """rmsnorm with its output in 8 bits, as quantize_c8 makes them from the unrounded norm -> (Xq8 [M,K] int8, a_scale fp32 [M]), or
+    (Xq8, a_scale, H) where there is a residual or H is given."""
+    if _fast is not None:
+        r = _fast.rmsnorm_quantize_c8(X, gamma, eps, residual, Xq8, a_scale, H)
+        if r is not None:
+            return r
+    M, K, ldx, ldr, g, H, ldh = _norm_arguments(X, gamma, residual, H)
+    if Xq8 is None:
+        Xq8 = _new_codes(M, K, X.device)
+    if a_scale is None:
+        a_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+    _check(lib().qvggt_rmsnorm_quantize_c8(_ptr(X), _ptr(residual), TYPES[X.dtype], ldx, ldr, M, K, g, eps, _ptr(H), ldh, _ptr(Xq8),
+                                           _rows(Xq8, M, K, torch.int8), _vector(a_scale, M), _stream()), "qvggt_rmsnorm_quantize_c8")
+    return (Xq8, a_scale) if H is None else (Xq8, a_scale, H)
+
+
+def linear_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, Wq8: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor | None = None,
+              dtype: torch.dtype = torch.bfloat16, Y: torch.Tensor | None = None) -> torch.Tensor:
+    """Product of 8-bit codes with scales for each token and channel: Xq8 [M,K], Wq8 [N,K] int8 (rows a multiple of 16 bytes apart),
+    a_scale fp32 [M], w_scale fp32 [N], bias [N] of the results' type or None -> Y [M,N] of `dtype` (or of Y's own, where Y is given).
+    A new Y has rows a multiple of 16 bytes apart (a view, where N is no such multiple)."""
+    if _fast is not None and dtype in TYPES:
+        r = _fast.linear_c8(Xq8, a_scale, Wq8, w_scale, bias, TYPES[dtype], Y)
+        if r is not None:
+            return r
+    assert Xq8.dim() == 2 and Wq8.dim() == 2
+    (M, K), N = Xq8.shape, Wq8.shape[0]
+    ldx, ldw = _rows(Xq8, M, K, torch.int8), _rows(Wq8, N, K, torch.int8)
+    if Y is None:
+        assert dtype in TYPES
+        step = 16 // dtype.itemsize
+        Y = torch.empty((M, (N + step - 1) // step * step), dtype=dtype, device=Xq8.device)[:, :N]
+    assert Y.dtype in TYPES
+    _check(lib().qvggt_linear_c8(_ptr(Xq8), ldx, _vector(a_scale, M), _ptr(Wq8), ldw, _vector(w_scale, N),
+                                 None if bias is None else _vector(bias, N, Y.dtype), M, N, K, _ptr(Y), TYPES[Y.dtype], _rows(Y, M, N, Y.dtype),
+                                 _stream()), "qvggt_linear_c8")
+    return Y

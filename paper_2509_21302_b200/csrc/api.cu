@@ -18,6 +18,13 @@ int device_is_sm100()
     return major == 10;
 }
 
+bool valid_type(int type) { return type == QVGGT_BF16 || type == QVGGT_FP16 || type == QVGGT_FP32; }
+
+// Rows of a matrix of the rotation-free path: any leading dimension from the row's length on, elements on their own boundaries.
+bool element_aligned(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == QVGGT_FP32 ? 4 : 2) == 0; }
+
+constexpr int MAX_ROWS = 2147483392, MAX_ROW = 131056;   // rows: whole tiles stay below 2^31; row length: 128 * 128 * K stays below 2^31
+
 // The handle's device is current.  `idle`: no device work uses the handle's memory any more.  Where that is not known (a
 // synchronisation that failed, as under a stream capture), the memory is not kept for the next handle.
 void release(qvggt_weights *w, bool idle)
@@ -376,6 +383,91 @@ void qvggt_free_weights(qvggt_weights_t *w)
     if (cur != owner) cudaSetDevice(cur);
 }
 
+int qvggt_quantize_c8(const void *X, int type, long long ldx, int M, int K, signed char *Xq8, long long ldq, float *a_scale, void *cuda_stream)
+{
+    if (!valid_type(type)) return QVGGT_ERR_UNSUPPORTED;
+    if (M < 0 || M > MAX_ROWS || K < 1 || K > MAX_ROW) return QVGGT_ERR_SHAPE;
+    if (M == 0) return QVGGT_OK;
+    if (!X || !Xq8 || !a_scale) return QVGGT_ERR_NULL;
+    if (ldx < K || ldq < K) return QVGGT_ERR_SHAPE;
+    if (!element_aligned(X, type) || !element_aligned(a_scale, QVGGT_FP32)) return QVGGT_ERR_ALIGN;
+    if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    cudaError_t e = qvggt_launch_rows(type, X, ldx, nullptr, 0, M, K, nullptr, 0.0f, nullptr, 0, nullptr, 0, Xq8, ldq, a_scale, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+int qvggt_dequantize_c8(const signed char *Xq8, long long ldq, const float *a_scale, int M, int K, void *Y, int type, long long ldy, void *cuda_stream)
+{
+    if (!valid_type(type)) return QVGGT_ERR_UNSUPPORTED;
+    if (M < 0 || M > MAX_ROWS || K < 1 || K > MAX_ROW) return QVGGT_ERR_SHAPE;
+    if (M == 0) return QVGGT_OK;
+    if (!Xq8 || !a_scale || !Y) return QVGGT_ERR_NULL;
+    if (ldq < K || ldy < K) return QVGGT_ERR_SHAPE;
+    if (!element_aligned(Y, type) || !element_aligned(a_scale, QVGGT_FP32)) return QVGGT_ERR_ALIGN;
+    if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    cudaError_t e = qvggt_launch_dequantize(type, Xq8, ldq, a_scale, M, K, Y, ldy, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+// What the two forms of the norm share: the checks of everything but the output.
+static int check_rmsnorm(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K, const float *gamma, float eps,
+                         const void *H, long long ldh)
+{
+    if (!valid_type(type)) return QVGGT_ERR_UNSUPPORTED;
+    if (M < 0 || M > MAX_ROWS || K < 1 || K > MAX_ROW) return QVGGT_ERR_SHAPE;
+    if (!(eps >= 0.0f && eps <= 3.4e38f)) return QVGGT_ERR_UNSUPPORTED;
+    if (M == 0) return QVGGT_OK;
+    if (!X || !gamma) return QVGGT_ERR_NULL;
+    if (ldx < K || (residual && ldr < K) || (H && ldh < K)) return QVGGT_ERR_SHAPE;
+    if (!element_aligned(X, type) || !element_aligned(residual, type) || !element_aligned(H, type) || !element_aligned(gamma, QVGGT_FP32)) return QVGGT_ERR_ALIGN;
+    return QVGGT_OK;
+}
+
+int qvggt_rmsnorm(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K, const float *gamma, float eps,
+                  void *H, long long ldh, void *Y, long long ldy, void *cuda_stream)
+{
+    const int bad = check_rmsnorm(X, residual, type, ldx, ldr, M, K, gamma, eps, H, ldh);
+    if (bad != QVGGT_OK || M == 0) return bad;
+    if (!Y) return QVGGT_ERR_NULL;
+    if (ldy < K) return QVGGT_ERR_SHAPE;
+    if (!element_aligned(Y, type)) return QVGGT_ERR_ALIGN;
+    if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    cudaError_t e = qvggt_launch_rows(type, X, ldx, residual, ldr, M, K, gamma, eps, H, ldh, Y, ldy, nullptr, 0, nullptr, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+int qvggt_rmsnorm_quantize_c8(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K, const float *gamma, float eps,
+                              void *H, long long ldh, signed char *Xq8, long long ldq, float *a_scale, void *cuda_stream)
+{
+    const int bad = check_rmsnorm(X, residual, type, ldx, ldr, M, K, gamma, eps, H, ldh);
+    if (bad != QVGGT_OK || M == 0) return bad;
+    if (!Xq8 || !a_scale) return QVGGT_ERR_NULL;
+    if (ldq < K) return QVGGT_ERR_SHAPE;
+    if (!element_aligned(a_scale, QVGGT_FP32)) return QVGGT_ERR_ALIGN;
+    if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    cudaError_t e = qvggt_launch_rows(type, X, ldx, residual, ldr, M, K, gamma, eps, H, ldh, nullptr, 0, Xq8, ldq, a_scale, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw, const float *w_scale,
+                    const void *bias, int M, int N, int K, void *Y, int type, long long ldy, void *cuda_stream)
+{
+    if (!valid_type(type)) return QVGGT_ERR_UNSUPPORTED;
+    if (M < 0 || M > MAX_ROWS || N < 1 || K < 1 || K > MAX_ROW) return QVGGT_ERR_SHAPE;
+    if (M == 0) return QVGGT_OK;
+    if (!Xq8 || !a_scale || !Wq8 || !w_scale || !Y) return QVGGT_ERR_NULL;
+    if (ldx < K || ldw < K || ldy < N) return QVGGT_ERR_SHAPE;
+    if (!aligned16(Xq8) || ldx % 16 != 0 || !aligned16(Wq8) || ldw % 16 != 0 || !element_aligned(a_scale, QVGGT_FP32) || !element_aligned(w_scale, QVGGT_FP32) ||
+        !element_aligned(bias, type) || !element_aligned(Y, type))
+        return QVGGT_ERR_ALIGN;
+    if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    QvggtLinear p = {};
+    p.Xq8 = Xq8; p.Wq8 = Wq8; p.ldx = ldx; p.ldw = ldw; p.ldy = ldy; p.a_scale = a_scale; p.w_scale = w_scale; p.bias = bias; p.Y = Y;
+    p.M = M; p.N = N; p.K = K; p.type = type;
+    cudaError_t e = qvggt_launch_linear_few(p, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
 int qvggt_weights_view(const qvggt_weights_t *w, const unsigned char **Wq, const float **w_scale, const float **amul,
                        const void **bias_bf16, int *N, int *K)
 {
@@ -425,9 +517,9 @@ const char *qvggt_status_string(int status)
     switch (status) {
         case QVGGT_OK: return "ok";
         case QVGGT_ERR_NULL: return "a required pointer is NULL";
-        case QVGGT_ERR_SHAPE: return "unsupported shape (K must be 1024 or 4096, N a multiple of 128, M >= 0, ld >= row length)";
-        case QVGGT_ERR_ALIGN: return "pointer or leading dimension violates the 16-byte alignment rule";
-        case QVGGT_ERR_UNSUPPORTED: return "unsupported option or device (group must be 0 or 128; device must be sm_100)";
+        case QVGGT_ERR_SHAPE: return "unsupported shape (ld >= row length, M >= 0; on the rotated path K must be 1024 or 4096, N a multiple of 128)";
+        case QVGGT_ERR_ALIGN: return "pointer or leading dimension violates the alignment rule (16 bytes, where the entry point says no other)";
+        case QVGGT_ERR_UNSUPPORTED: return "unsupported option, type or device (group must be 0 or 128; device must be sm_100)";
         case QVGGT_ERR_CUDA: return "a CUDA runtime call failed";
         case QVGGT_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
         case QVGGT_ERR_NOMEM: return "out of memory";

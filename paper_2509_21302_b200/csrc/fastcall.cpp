@@ -367,6 +367,164 @@ PyObject *prepare_weights(PyObject *, PyObject *const *args, Py_ssize_t n)
     QVGGT_GUARD_END
 }
 
+// ---------------------------------------------------------------- the rotation-free 8-bit path
+int type_code(ScalarType t) { return t == at::kBFloat16 ? QVGGT_BF16 : t == at::kHalf ? QVGGT_FP16 : t == at::kFloat ? QVGGT_FP32 : -1; }
+ScalarType scalar_type(int64_t code) { return code == QVGGT_BF16 ? at::kBFloat16 : code == QVGGT_FP16 ? at::kHalf : at::kFloat; }
+int64_t up(int64_t n, int64_t step) { return (n + step - 1) / step * step; }
+
+// Matrices and vectors of one call, all of which have to lie on the current device.
+struct Plain {
+    Args in;
+    c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream();
+    Plain(PyObject *const *args, Py_ssize_t n) : in{args, n} {}
+
+    // Unit stride along a row.
+    const Tensor &matrix(bool optional = false)
+    {
+        const Tensor &t = in.tensor(optional);
+        if (in.ok && t.defined() && !(t.dim() == 2 && (t.size(1) <= 1 || t.stride(1) == 1) && t.get_device() == st.device_index())) in.ok = false;
+        return t;
+    }
+    const Tensor &matrix(ScalarType type, int64_t M, int64_t K, bool optional)
+    {
+        const Tensor &t = matrix(optional);
+        if (in.ok && t.defined() && !(t.scalar_type() == type && t.size(0) == M && t.size(1) == K)) in.ok = false;
+        return t;
+    }
+    const Tensor &vector(ScalarType type, int64_t n, bool optional)
+    {
+        const Tensor &t = in.exact(type, n, -1, optional);
+        if (in.ok && t.defined() && t.get_device() != st.device_index()) in.ok = false;
+        return t;
+    }
+    static int64_t ld(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : up(t.size(1), 16); }
+    // `given`, or a new matrix whose rows are a multiple of 16 bytes apart.
+    static Tensor or_new(const Tensor &given, int64_t M, int64_t K, const at::TensorOptions &options, int64_t step)
+    {
+        if (given.defined()) return given;
+        const int64_t width = up(K, step);
+        const Tensor t = at::empty({M, width}, options);
+        return width == K ? t : t.as_strided({M, K}, {width, 1});
+    }
+    bool sizes(int64_t M, int64_t K) { return in.ok && M <= INT32_MAX && K >= 1 && K <= INT32_MAX; }
+};
+
+// (X, Xq8, a_scale)
+PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    QVGGT_GUARD_BEGIN
+    Plain p(args, n);
+    const Tensor &X = p.matrix();
+    if (!p.in.ok || !p.sizes(X.size(0), X.size(1)) || type_code(X.scalar_type()) < 0) Py_RETURN_NONE;
+    const int64_t M = X.size(0), K = X.size(1);
+    const Tensor &xq = p.matrix(at::kChar, M, K, true), &as = p.vector(at::kFloat, M, true);
+    if (!p.in.done()) Py_RETURN_NONE;
+    const Tensor q = Plain::or_new(xq, M, K, X.options().dtype(at::kChar), 16), a = as.defined() ? as : at::empty({M}, X.options().dtype(at::kFloat));
+    const void *x = X.data_ptr();
+    S8 *qp = static_cast<S8 *>(q.data_ptr());
+    float *ap = static_cast<float *>(a.data_ptr());
+    const int type = type_code(X.scalar_type());
+    const int64_t ldx = Plain::ld(X), ldq = Plain::ld(q);
+    void *st = p.st.stream();
+    if (without_gil([&] { return qvggt_quantize_c8(x, type, ldx, (int)M, (int)K, qp, ldq, ap, st); }) != QVGGT_OK) Py_RETURN_NONE;
+    return release_items(PyTuple_Pack(2, wrap(xq, q, args[1]), wrap(as, a, args[2])));
+    QVGGT_GUARD_END
+}
+
+// (Xq8, a_scale, type, Y)
+PyObject *dequantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    QVGGT_GUARD_BEGIN
+    Plain p(args, n);
+    const Tensor &xq = p.matrix();
+    if (!p.in.ok || !p.sizes(xq.size(0), xq.size(1)) || xq.scalar_type() != at::kChar) Py_RETURN_NONE;
+    const int64_t M = xq.size(0), K = xq.size(1);
+    const Tensor &as = p.vector(at::kFloat, M, false);
+    const int64_t wanted = p.in.integer();
+    const Tensor &given = p.matrix(true);
+    if (!p.in.done() || (given.defined() && (given.size(0) != M || given.size(1) != K))) Py_RETURN_NONE;
+    const Tensor y = given.defined() ? given : at::empty({M, K}, xq.options().dtype(scalar_type(wanted)));
+    const int type = type_code(y.scalar_type());
+    if (type < 0) Py_RETURN_NONE;
+    const S8 *qp = static_cast<const S8 *>(xq.data_ptr());
+    const float *ap = static_cast<const float *>(as.data_ptr());
+    void *yp = y.data_ptr(), *st = p.st.stream();
+    const int64_t ldq = Plain::ld(xq), ldy = Plain::ld(y);
+    if (without_gil([&] { return qvggt_dequantize_c8(qp, ldq, ap, (int)M, (int)K, yp, type, ldy, st); }) != QVGGT_OK) Py_RETURN_NONE;
+    return wrap(given, y, args[3]);
+    QVGGT_GUARD_END
+}
+
+// (X, gamma, eps, residual, Y, H), QUANT: (X, gamma, eps, residual, Xq8, a_scale, H)
+template <bool QUANT>
+PyObject *rmsnorm_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    QVGGT_GUARD_BEGIN
+    Plain p(args, n);
+    const Tensor &X = p.matrix();
+    if (!p.in.ok || !p.sizes(X.size(0), X.size(1)) || type_code(X.scalar_type()) < 0) Py_RETURN_NONE;
+    const int64_t M = X.size(0), K = X.size(1);
+    const ScalarType T = X.scalar_type();
+    const Tensor &gamma = p.vector(at::kFloat, K, false);
+    const float eps = (float)p.in.real();
+    const Tensor &R = p.matrix(T, M, K, true), &out = p.matrix(QUANT ? at::kChar : T, M, K, true);
+    static const Tensor none;
+    const Tensor &as = QUANT ? p.vector(at::kFloat, M, true) : none, &hg = p.matrix(T, M, K, true);
+    if (!p.in.done()) Py_RETURN_NONE;
+    const bool sum = R.defined() || hg.defined();
+    const Tensor h = hg.defined() || !sum ? hg : at::empty({M, K}, X.options());
+    const Tensor y = QUANT ? Plain::or_new(out, M, K, X.options().dtype(at::kChar), 16) : out.defined() ? out : at::empty({M, K}, X.options());
+    const Tensor a = !QUANT || as.defined() ? as : at::empty({M}, X.options().dtype(at::kFloat));
+    const void *x = X.data_ptr(), *r = R.defined() ? R.data_ptr() : nullptr;
+    const float *gp = static_cast<const float *>(gamma.data_ptr());
+    void *hp = sum ? h.data_ptr() : nullptr, *yp = y.data_ptr(), *st = p.st.stream();
+    float *ap = QUANT ? static_cast<float *>(a.data_ptr()) : nullptr;
+    const int type = type_code(T);
+    const int64_t ldx = Plain::ld(X), ldr = r ? Plain::ld(R) : 0, ldh = sum ? Plain::ld(h) : 0, ldy = Plain::ld(y);
+    const int status = without_gil([&] {
+        return QUANT ? qvggt_rmsnorm_quantize_c8(x, r, type, ldx, ldr, (int)M, (int)K, gp, eps, hp, ldh, static_cast<S8 *>(yp), ldy, ap, st)
+                     : qvggt_rmsnorm(x, r, type, ldx, ldr, (int)M, (int)K, gp, eps, hp, ldh, yp, ldy, st);
+    });
+    if (status != QVGGT_OK) Py_RETURN_NONE;
+    PyObject *oy = wrap(out, y, args[4]);
+    if (QUANT) {
+        PyObject *oa = wrap(as, a, args[5]);
+        return release_items(sum ? PyTuple_Pack(3, oy, oa, wrap(hg, h, args[6])) : PyTuple_Pack(2, oy, oa));
+    }
+    return sum ? release_items(PyTuple_Pack(2, oy, wrap(hg, h, args[5]))) : oy;
+    QVGGT_GUARD_END
+}
+
+// (Xq8, a_scale, Wq8, w_scale, bias, type, Y)
+PyObject *linear_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    QVGGT_GUARD_BEGIN
+    Plain p(args, n);
+    const Tensor &xq = p.matrix();
+    if (!p.in.ok || !p.sizes(xq.size(0), xq.size(1)) || xq.scalar_type() != at::kChar) Py_RETURN_NONE;
+    const int64_t M = xq.size(0), K = xq.size(1);
+    const Tensor &as = p.vector(at::kFloat, M, false), &wq = p.matrix();
+    if (!p.in.ok || wq.scalar_type() != at::kChar || wq.size(1) != K || !p.sizes(wq.size(0), K)) Py_RETURN_NONE;
+    const int64_t N = wq.size(0);
+    const Tensor &ws = p.vector(at::kFloat, N, false), &bias = p.in.tensor(true);
+    const int64_t wanted = p.in.integer();
+    const Tensor &given = p.matrix(true);
+    if (!p.in.done() || (given.defined() && (given.size(0) != M || given.size(1) != N))) Py_RETURN_NONE;
+    const ScalarType T = given.defined() ? given.scalar_type() : scalar_type(wanted);
+    const int type = type_code(T);
+    if (type < 0 || (bias.defined() && !(bias.scalar_type() == T && bias.dim() == 1 && bias.size(0) == N && bias.is_contiguous() && bias.get_device() == p.st.device_index())))
+        Py_RETURN_NONE;
+    const Tensor y = Plain::or_new(given, M, N, xq.options().dtype(T), type == QVGGT_FP32 ? 4 : 8);
+    const S8 *qp = static_cast<const S8 *>(xq.data_ptr()), *wp = static_cast<const S8 *>(wq.data_ptr());
+    const float *ap = static_cast<const float *>(as.data_ptr()), *sp = static_cast<const float *>(ws.data_ptr());
+    const void *bp = bias.defined() ? bias.data_ptr() : nullptr;
+    void *yp = y.data_ptr(), *st = p.st.stream();
+    const int64_t ldx = Plain::ld(xq), ldw = Plain::ld(wq), ldy = Plain::ld(y);
+    if (without_gil([&] { return qvggt_linear_c8(qp, ldx, ap, wp, ldw, sp, bp, (int)M, (int)N, (int)K, yp, type, ldy, st); }) != QVGGT_OK) Py_RETURN_NONE;
+    return wrap(given, y, args[6]);
+    QVGGT_GUARD_END
+}
+
 // Copy of a device array as a new tensor on the current device (d1 < 0: one dimension), undefined for a null pointer.  The array lies
 // on the device of its handle, which need not be the current one.
 Tensor copy_array(const void *p, ScalarType type, int64_t d0, int64_t d1)
@@ -434,6 +592,11 @@ PyMethodDef methods[] = {
     FAST("w4a4_linear_c8_grouped", (linear_c8<qvggt_w4a4_linear_c8_grouped, true>)),
     FAST("w4a4_linear_c8_packed_weights", (linear_scratch<false>)),
     FAST("w4a4_linear_c8_expanded", (linear_scratch<true>)),
+    FAST("quantize_c8", quantize_rows),
+    FAST("dequantize_c8", dequantize_rows),
+    FAST("rmsnorm", rmsnorm_rows<false>),
+    FAST("rmsnorm_quantize_c8", rmsnorm_rows<true>),
+    FAST("linear_c8", linear_rows),
     FAST("calibrate_smooth", calibrate_smooth),
     FAST("prepare_weights", prepare_weights),
     FAST("weights_view", weights_view),

@@ -99,3 +99,20 @@ cudaError_t qvggt_launch_gemm_c8_expanded(const qvggt_weights *w, const signed c
 // One activation scale per token per 128 rotated channels on one-code-per-byte operands (a_scale [M, K/128]).
 cudaError_t qvggt_launch_gemm_c8_grouped(const qvggt_weights *w, const signed char *Xq8, const float *a_scale, int M, void *Y,
                                          long long ldy, int *acc_debug, cudaStream_t st);
+
+// rows_c8.cu: the row operators without rotation.  gamma: RMS norm in front (R, H: residual in, sum out, or nullptr), nullptr: none;
+// the output is Xq8 with scales, or Y where Xq8 is nullptr.  Leading dimensions in elements, rows >= 1.
+cudaError_t qvggt_launch_rows(int type, const void *X, long long ldx, const void *R, long long ldr, int M, int K, const float *gamma, float eps,
+                              void *H, long long ldh, void *Y, long long ldy, signed char *Xq8, long long ldq, float *scales, cudaStream_t st);
+cudaError_t qvggt_launch_dequantize(int type, const signed char *Xq8, long long ldq, const float *scales, int M, int K, void *Y, long long ldy, cudaStream_t st);
+
+// The integer product of qvggt_linear_c8; M >= 1, arguments checked.
+struct QvggtLinear {
+    const signed char *Xq8, *Wq8;
+    long long ldx, ldw, ldy;
+    const float *a_scale, *w_scale;
+    const void *bias;          // of the results' type, or nullptr
+    void *Y;
+    int M, N, K, type;
+};
+cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st);      // linear_few.cu
