@@ -321,6 +321,13 @@ int qvggt_rmsnorm_quantize_c8(const void *X, const void *residual, int type, lon
 int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw,
                     const float *w_scale, const void *bias, int M, int N, int K, void *Y, int type, long long ldy, void *cuda_stream);
 
+/*
+ * What qvggt_device_status is for a handle, for qvggt_linear_c8, which has none: synchronises `cuda_stream`, then reads the current
+ * device's status word into *code (HOST pointer).  0 = no device-side wait has expired since the library was loaded; otherwise the
+ * positive code of the first wait that gave up (the results of that call are not all written), and QVGGT_ERR_DEVICE_TIMEOUT.
+ */
+int qvggt_linear_status(void *cuda_stream, int *code);
+
 /* Frees the handle and its device memory (synchronises the device first).  At most 64 MB per device stay with the library for
  * the next handle; they go back to the driver when an allocation of the library fails.  NULL is allowed. */
 void qvggt_free_weights(qvggt_weights_t *w);

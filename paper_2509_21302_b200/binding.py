@@ -31,7 +31,8 @@ EXPORTS = ("qvggt_prepare_weights", "qvggt_rotate_smooth_quantize", "qvggt_w4a4_
            "qvggt_gelu_rotate_smooth_quantize_c8", "qvggt_w4a4_linear_c8_packed_weights",
            "qvggt_rotate_smooth_quantize_c8_grouped", "qvggt_w4a4_linear_c8_grouped",
            "qvggt_rotate_smooth_quantize_c8_expand", "qvggt_w4a4_linear_c8_expanded",
-           "qvggt_quantize_c8", "qvggt_dequantize_c8", "qvggt_rmsnorm", "qvggt_rmsnorm_quantize_c8", "qvggt_linear_c8")
+           "qvggt_quantize_c8", "qvggt_dequantize_c8", "qvggt_rmsnorm", "qvggt_rmsnorm_quantize_c8", "qvggt_linear_c8",
+           "qvggt_linear_status")
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # QVGGT_BF16, QVGGT_FP16, QVGGT_FP32
 PREP_C8 = 1   # QVGGT_PREP_C8: keep an int8 [N, K] copy of the weight codes for the *_c8 entry points
 PREP_W8A8 = 2  # QVGGT_PREP_W8A8: 8-bit codes (one per byte only)
@@ -91,6 +92,7 @@ def lib() -> ctypes.CDLL:
         L.qvggt_rmsnorm.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp]
         L.qvggt_rmsnorm_quantize_c8.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp, vp]
         L.qvggt_linear_c8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
+        L.qvggt_linear_status.argtypes = [vp, ctypes.POINTER(i32)]
         L.qvggt_status_string.argtypes = [i32]
         L.qvggt_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -633,3 +635,12 @@ def linear_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, Wq8: torch.Tensor, w_sca
                                  None if bias is None else _vector(bias, N, Y.dtype), M, N, K, _ptr(Y), TYPES[Y.dtype], _rows(Y, M, N, Y.dtype),
                                  _stream()), "qvggt_linear_c8")
     return Y
+
+
+def linear_status() -> int:
+    """The current device's status word of linear_c8 (0: no device-side wait has expired); synchronises the current stream."""
+    code = ctypes.c_int(0)
+    st = lib().qvggt_linear_status(_stream(), ctypes.byref(code))
+    if st not in (OK, -6):
+        raise QvggtError(st, "qvggt_linear_status")
+    return code.value

@@ -464,8 +464,15 @@ int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale,
     QvggtLinear p = {};
     p.Xq8 = Xq8; p.Wq8 = Wq8; p.ldx = ldx; p.ldw = ldw; p.ldy = ldy; p.a_scale = a_scale; p.w_scale = w_scale; p.bias = bias; p.Y = Y;
     p.M = M; p.N = N; p.K = K; p.type = type;
-    cudaError_t e = qvggt_launch_linear_few(p, static_cast<cudaStream_t>(cuda_stream));
+    cudaError_t e = qvggt_launch_linear(p, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+int qvggt_linear_status(void *cuda_stream, int *code)
+{
+    if (!code) return QVGGT_ERR_NULL;
+    if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess || qvggt_read_linear_status(code) != cudaSuccess) return QVGGT_ERR_CUDA;
+    return *code == 0 ? QVGGT_OK : QVGGT_ERR_DEVICE_TIMEOUT;
 }
 
 int qvggt_weights_view(const qvggt_weights_t *w, const unsigned char **Wq, const float **w_scale, const float **amul,

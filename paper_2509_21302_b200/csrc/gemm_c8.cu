@@ -31,6 +31,7 @@
 
 #include <type_traits>
 
+#include "element.cuh"
 #include "gemm_c8_plan.cuh"
 #include "gemm_common.cuh"
 #include "qvggt_internal.cuh"
@@ -54,7 +55,6 @@ constexpr int TMEM_COLS = ACC_BUFS * ACC_COLS;
 
 constexpr int STG_WARP = 16 * 2 * UNIT;                // staging of one epilogue warp: 16 rows x 64 bf16, 128-byte swizzled
 constexpr int OFF_OPS = EPI_WARPS * STG_WARP;          // operands: [resident token rows,] ring of stages (1024-byte aligned)
-static_assert(EPI_WARPS * 4 * STG_WARP <= OPS_BYTES, "the last tile is staged where the operands were");
 constexpr int OFF_BAR = OFF_OPS + OPS_BYTES;           // full[MAX_STAGES] empty[MAX_STAGES] tfull[2] tempty[2]
 constexpr int NBARS = 2 * MAX_STAGES + 2 * ACC_BUFS;
 constexpr int OFF_TMEM = OFF_BAR + NBARS * 8;
@@ -75,17 +75,106 @@ struct StageRing {
     }
 };
 
+// What a launch multiplies and where the results go.  HANDLE: a weights handle's layer (N a multiple of 128, K of 128, bf16 results, the
+// rounding of every operation of the epilogue fixed by the interface).  The other forms are qvggt_linear_c8: any N and K (tiles and stages
+// beyond them are filled with zeros by TMA, parameters of channels beyond N are not read), results and bias of one type,
+// fma(acc, a_scale * w_scale, bias) in the epilogue; ROWS_*: results whose rows do not begin on 16-byte boundaries, which no TMA store takes.
+enum Form { HANDLE, FORM_BF16, FORM_FP16, FORM_FP32, ROWS_BF16, ROWS_FP16, ROWS_FP32 };
+template <int FORM> struct ResultType { using T = __nv_bfloat16; };
+template <> struct ResultType<FORM_FP16> { using T = __half; };
+template <> struct ResultType<ROWS_FP16> { using T = __half; };
+template <> struct ResultType<FORM_FP32> { using T = float; };
+template <> struct ResultType<ROWS_FP32> { using T = float; };
+
+__device__ int linear_status;          // the status word of the launches without a handle
+
+// 16 rows x 64 channels as 16x256b fragments (see gemmc::finish_16x64_tma): fma(float(acc), fl(a_scale * w_scale), bias) in T, staged in the
+// warp's 2 KB (`stg`; 128-byte swizzle) and stored: by TMA, or by ordinary stores of neighbouring elements, rows from Y on with
+// stride ldy, of which `rows` x `cols` exist.  Ordinary stores take the ROWS forms and the piece that N ends in where N elements are no
+// multiple of 16 bytes: a TMA store writes whole 16 bytes there, over what lies behind the row.  fp32 takes two stages of 32 channels each,
+// 2 KB apart where stg_next is not 0.
+template <class T, bool ROWS>
+__device__ __forceinline__ void finish_16x64_any(const uint32_t (&raw)[32], const uint64_t (&as2)[2], const uint64_t (&w2)[8], const uint32_t (&c0)[8], const uint32_t (&c1)[8],
+                                                 unsigned char *stg, uint32_t stg_addr, uint32_t stg_next, bool reused, const void *map_y, int x, int y, bool issue, int lane, uint64_t policy,
+                                                 T *Y, long long ldy, int rows, int cols)
+{
+    constexpr int HALVES = sizeof(T) == 4 ? 2 : 1, COLS = 64 / HALVES;
+    const int t = lane & 3;
+#pragma unroll
+    for (int half = 0; half < HALVES; ++half) {
+        float z[8 / HALVES][2][2];
+#pragma unroll
+        for (int i = 0; i < 8 / HALVES; ++i) {
+            const int b = half * (8 / HALVES) + i;
+            uint64_t c2;
+            if constexpr (sizeof(T) == 4) {
+                c2 = ptx::f32x2_pack(__uint_as_float(c0[b]), __uint_as_float(c1[b]));
+            } else {
+                const float2 f = element::unpack2<T>(c0[b]);
+                c2 = ptx::f32x2_pack(f.x, f.y);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                ptx::f32x2_unpack(ptx::f32x2_fma(ptx::f32x2_pack(static_cast<float>(static_cast<int>(raw[4 * b + 2 * h])), static_cast<float>(static_cast<int>(raw[4 * b + 2 * h + 1]))),
+                                                 ptx::f32x2_mul(as2[h], w2[b]), c2), z[i][h][0], z[i][h][1]);
+        }
+        const uint32_t at = half * stg_next;
+        const int left = cols - half * COLS;
+        const bool ordinary = ROWS || (left < COLS && left * (int)sizeof(T) % 16 != 0);
+        if ((reused || (half && !stg_next)) && !ROWS && lane == 0) ptx::tma_store_wait_read<0>();
+        __syncwarp();                       // the previous rows have left the staging tile
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t st_row = stg_addr + (lane & 15) * 128;
+#pragma unroll
+            for (int b = 0; b < 8; b += 2)  // matrices (rows 0-7, block b), (rows 8-15, b), (0-7, b + 1), (8-15, b + 1)
+                ptx::stmatrix_x4(st_row + (((b + (lane >> 4)) ^ (lane & 7)) << 4), element::pack2<T>(z[b][0][0], z[b][0][1]), element::pack2<T>(z[b][1][0], z[b][1][1]),
+                                 element::pack2<T>(z[b + 1][0][0], z[b + 1][0][1]), element::pack2<T>(z[b + 1][1][0], z[b + 1][1][1]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = (lane >> 2) + 8 * h;
+                    *reinterpret_cast<float2 *>(stg + at + r * 128 + (((2 * i + (t >> 1)) ^ (r & 7)) << 4) + 8 * (t & 1)) = make_float2(z[i][h][0], z[i][h][1]);
+                }
+        }
+        if (ordinary) {
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+#pragma unroll
+                for (int k = 0; k < COLS / 32; ++k) {
+                    const int c = lane + 32 * k, byte = c * (int)sizeof(T);
+                    const T v = *reinterpret_cast<const T *>(stg + at + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+                    if (r < rows && c < left) Y[r * ldy + half * COLS + c] = v;
+                }
+            __syncwarp();
+        } else {
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && issue && left > 0) {
+                ptx::tma_store_2d(map_y, stg_addr + at, x + half * COLS, y, policy);
+                ptx::tma_store_commit();
+            }
+        }
+    }
+}
+
 // RESIDENT (K = 1024): all eight K-blocks of a tile's token rows stay in shared memory for as long as the worker's tiles share
 // them, and only weight rows stream.
 // DUMP: also write the int32 sums to acc_debug (its own instantiation keeps that code out of the production kernel).
 // wait_limit: bound of every device-side wait, in cycles.  skip_loads: the TMA producers issue nothing, so that the
 // first wait for operands runs out (used only to exercise the timeout path; no asynchronous operation is in flight).
-template <bool RESIDENT, bool DUMP>
+template <bool RESIDENT, bool DUMP, int FORM>
 __global__ void __launch_bounds__(THREADS, 1)
 gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_wu,
-               const __grid_constant__ CUtensorMap map_y, const __grid_constant__ Plan plan, const float *__restrict__ a_scale, const float *__restrict__ w_scale, const uint16_t *__restrict__ bias,
-               int *__restrict__ acc_debug, int M, int N, int K, int *status, long long wait_limit, int skip_loads)
+               const __grid_constant__ CUtensorMap map_y, const __grid_constant__ Plan plan, const float *__restrict__ a_scale, const float *__restrict__ w_scale, const void *__restrict__ bias_,
+               void *__restrict__ Y, long long ldy, int *__restrict__ acc_debug, int M, int N, int K, int *status_, long long wait_limit, int skip_loads)
 {
+    using T = typename ResultType<FORM>::T;
+    constexpr bool ROWS = FORM >= ROWS_BF16;
+    const uint16_t *__restrict__ bias = static_cast<const uint16_t *>(bias_);      // (HANDLE)
+    int *status = FORM == HANDLE ? status_ : &linear_status;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sbase = ptx::smem_addr(smem);
@@ -99,7 +188,7 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();                       // 0 = leader of the pair
-    const int KB = RESIDENT ? RES_KB : K / BK;
+    const int KB = RESIDENT ? RES_KB : FORM == HANDLE ? K / BK : (K + BK - 1) / BK;
 
     // full: the leader's arrive.expect_tx (bytes of both CTAs); empty, tfull: tcgen05.commit; tempty: the epilogue warps of both CTAs
     if (threadIdx.x < NBARS) {
@@ -135,6 +224,8 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 
     if (warp < EPI_WARPS) {
         // ------------------------------------------------------------ epilogue
+        constexpr int PIECES = 2 * sizeof(T);              // staging tiles of a warp's part of a tile: 4 of 16 x 64 elements in 16 bits
+        static_assert(EPI_WARPS * PIECES * STG_WARP <= OPS_BYTES, "the last tile is staged where the operands were");
         const int quarter = warp & 3, part = warp >> 2;    // TMEM lane quarter; of the units, part 0 takes the first half
         const uint32_t stg_addr = sbase + warp * STG_WARP;
         const uint32_t leader_tempty = ptx::map_to_cta(bar_tempty, 0);
@@ -152,14 +243,26 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             // Scales and biases of channels 8 e + 2 (lane mod 4) and + 1 of each unit, in the layout of the accumulator fragments and
             // straight into registers: read from shared memory for every 16 rows they took as much of its bandwidth as the outputs.
             uint64_t w2[2][8];
-            uint32_t c2[2][8];
+            uint32_t c2[2][8], c2_more[2][8];                      // biases: two in a word; fp32: the second of a pair in c2_more
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int n = n0 + (k < units ? k * UNIT : 0) + 8 * e + 2 * (lane & 3);
-                    w2[k][e] = __ldg(reinterpret_cast<const unsigned long long *>(w_scale + n));
-                    c2[k][e] = bias ? __ldg(reinterpret_cast<const uint32_t *>(bias + n)) : 0u;
+                    if constexpr (FORM == HANDLE) {
+                        w2[k][e] = __ldg(reinterpret_cast<const unsigned long long *>(w_scale + n));
+                        c2[k][e] = bias ? __ldg(reinterpret_cast<const uint32_t *>(bias + n)) : 0u;
+                    } else {                                       // off wide boundaries and up to N, where nothing is read
+                        w2[k][e] = ptx::f32x2_pack(n < N ? __ldg(w_scale + n) : 0.0f, n + 1 < N ? __ldg(w_scale + n + 1) : 0.0f);
+                        const T *b = static_cast<const T *>(bias_);
+                        if constexpr (sizeof(T) == 4) {
+                            c2[k][e] = b && n < N ? __float_as_uint(__ldg(b + n)) : 0u;
+                            c2_more[k][e] = b && n + 1 < N ? __float_as_uint(__ldg(b + n + 1)) : 0u;
+                        } else {
+                            const unsigned short *u = reinterpret_cast<const unsigned short *>(b);
+                            c2[k][e] = (b && n < N ? __ldg(u + n) : 0u) | (b && n + 1 < N ? static_cast<uint32_t>(__ldg(u + n + 1)) << 16 : 0u);
+                        }
+                    }
                 }
             uint64_t as2[2][2];                                // rows lane / 4 + 8 h of the warp's 16 u .. 16 u + 15
 #pragma unroll
@@ -178,7 +281,7 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             // where the others wait for the store of the piece before them (0.13 us of a launch of one tile per worker, us: K = 1024,
             // N = 4096, 600 rows 6.03 / 5.90; K = 4096, N = 1024, 4122 rows 13.54 / 13.40).
             const bool last = t == my_tiles - 1;
-            const uint32_t stg = last ? ops + warp * (4 * STG_WARP) : stg_addr, stg_next = last ? STG_WARP : 0;
+            const uint32_t stg = last ? ops + warp * (PIECES * STG_WARP) : stg_addr, stg_next = last ? STG_WARP : 0;
             if (alive) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -198,7 +301,13 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                         for (int u = 0; u < 2; ++u) {
                             const int m = m0 + 16 * u, n = n0 + k * UNIT;
                             if (by_rows && u != part) continue;
-                            gemmc::finish_16x64_tma(raw[u], as2[u], w2[k], c2[k], stg + (2 * k + u) * stg_next, !last, &map_y, n, m, m < M, lane, one2, policy);
+                            if constexpr (FORM == HANDLE) {
+                                gemmc::finish_16x64_tma(raw[u], as2[u], w2[k], c2[k], stg + (2 * k + u) * stg_next, !last, &map_y, n, m, m < M, lane, one2, policy);
+                            } else {
+                                const uint32_t at = stg + (PIECES / 2 * k + PIECES / 4 * u) * stg_next;
+                                finish_16x64_any<T, ROWS>(raw[u], as2[u], w2[k], c2[k], c2_more[k], smem + (at - sbase), at, stg_next, !last, &map_y, n, m, m < M, lane, policy,
+                                                          static_cast<T *>(Y) + (long long)m * ldy + n, ldy, M - m, N - n);
+                            }
                             if (DUMP && acc_debug) gemmc::dump_16x64<0>(acc_debug + (long long)m * N + n, N, raw[u], M - m, lane);
                         }
                     }
@@ -590,22 +699,37 @@ __global__ void __launch_bounds__(256) unpack_w4_kernel(const uint4 *__restrict_
     qvggt_unpack_w4_item(packed, out, i);
 }
 
-template <bool RESIDENT, bool DUMP>
-cudaError_t launch_plan(const qvggt_weights *w, const signed char *wq8, const signed char *Xq8, const float *a_scale, int M, void *Y, long long ldy,
-                        int *acc_debug, cudaStream_t st, long long wait_limit, int skip_loads)
+// One product, however it is called.
+struct Call {
+    const signed char *x, *w;
+    long long ldx, ldw;
+    const float *a_scale, *w_scale;
+    const void *bias;
+    int M, N, K;
+    void *Y;
+    long long ldy;
+    int *acc_debug, *status;
+    long long wait_limit;
+    int skip_loads;
+};
+
+template <bool RESIDENT, bool DUMP, int FORM>
+cudaError_t launch_plan(const Call &c, cudaStream_t st)
 {
+    using T = typename ResultType<FORM>::T;
+    constexpr CUtensorMapDataType y_type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     static QvggtPerDevice cache;
     int workers = 0;
-    cudaError_t e = qvggt_configure_kernel(gemm_c8_kernel<RESIDENT, DUMP>, THREADS, DYN_SMEM, 2, cache, &workers);
+    cudaError_t e = qvggt_configure_kernel(gemm_c8_kernel<RESIDENT, DUMP, FORM>, THREADS, DYN_SMEM, 2, cache, &workers);
     if (e != cudaSuccess) return e;
-    const int K = w->K, N = w->N;
-    const Plan plan = make_plan(M, N, K, workers, &workers);
-    CUtensorMap map_x, map_w, map_wu, map_y;
-    if (!qvggt_make_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, Xq8, K, M, K, BK, BM, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !qvggt_make_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, wq8, K, N, K, BK, plan.wide * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !qvggt_make_map(&map_wu, CU_TENSOR_MAP_DATA_TYPE_UINT8, wq8, K, N, K, BK, plan.cut * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !qvggt_make_map(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, Y, N, M, (uint64_t)ldy * 2, UNIT, 16, CU_TENSOR_MAP_SWIZZLE_128B))
+    const Plan plan = make_plan(c.M, c.N, c.K, workers, &workers);
+    CUtensorMap map_x, map_w, map_wu, map_y = {};
+    if (!qvggt_make_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.x, c.K, c.M, c.ldx, BK, BM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !qvggt_make_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.w, c.K, c.N, c.ldw, BK, plan.wide * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !qvggt_make_map(&map_wu, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.w, c.K, c.N, c.ldw, BK, plan.cut * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
+        (FORM >= ROWS_BF16 ? false : !qvggt_make_map(&map_y, y_type, c.Y, c.N, c.M, (uint64_t)c.ldy * sizeof(T), 128 / sizeof(T), 16, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorInvalidValue;
+    if (FORM >= ROWS_BF16) map_y = map_x;                 // prefetched, not used
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -618,16 +742,22 @@ cudaError_t launch_plan(const qvggt_weights *w, const signed char *wq8, const si
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, gemm_c8_kernel<RESIDENT, DUMP>, map_x, map_w, map_wu, map_y, plan, a_scale,
-                              (const float *)w->w_scale, (const uint16_t *)w->bias, acc_debug, M, N, K, w->status, wait_limit, skip_loads);
+    return cudaLaunchKernelEx(&cfg, gemm_c8_kernel<RESIDENT, DUMP, FORM>, map_x, map_w, map_wu, map_y, plan, c.a_scale, c.w_scale, c.bias, c.Y, c.ldy, c.acc_debug,
+                              c.M, c.N, c.K, c.status, c.wait_limit, c.skip_loads);
+}
+
+template <bool DUMP, int FORM>
+cudaError_t launch_form(const Call &c, cudaStream_t st)
+{
+    return has_resident_rows(c.K) ? launch_plan<true, DUMP, FORM>(c, st) : launch_plan<false, DUMP, FORM>(c, st);
 }
 
 template <bool DUMP>
 cudaError_t launch(const qvggt_weights *w, const signed char *wq8, const signed char *Xq8, const float *a_scale, int M, void *Y, long long ldy,
                    int *acc_debug, cudaStream_t st, long long wait_limit, int skip_loads)
 {
-    if (w->K == RES_KB * BK) return launch_plan<true, DUMP>(w, wq8, Xq8, a_scale, M, Y, ldy, acc_debug, st, wait_limit, skip_loads);
-    return launch_plan<false, DUMP>(w, wq8, Xq8, a_scale, M, Y, ldy, acc_debug, st, wait_limit, skip_loads);
+    const Call c = {Xq8, wq8, w->K, w->K, a_scale, w->w_scale, w->bias, M, w->N, w->K, Y, ldy, acc_debug, w->status, wait_limit, skip_loads};
+    return launch_form<DUMP, HANDLE>(c, st);
 }
 
 }  // namespace
@@ -696,3 +826,15 @@ cudaError_t qvggt_launch_gemm_c8_grouped(const qvggt_weights *w, const signed ch
     return (reinterpret_cast<uintptr_t>(a_scale) & 15u) == 0 ? grp::launch<false, true>(w, Xq8, a_scale, M, Y, ldy, acc_debug, st)
                                                             : grp::launch<false, false>(w, Xq8, a_scale, M, Y, ldy, acc_debug, st);
 }
+
+cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st)
+{
+    if (!can_plan(p.M, p.N)) return cudaErrorNotSupported;
+    const Call c = {p.Xq8, p.Wq8, p.ldx, p.ldw, p.a_scale, p.w_scale, p.bias, p.M, p.N, p.K, p.Y, p.ldy, nullptr, nullptr, ptx::kWaitLimitCycles, 0};
+    const bool tma = (reinterpret_cast<uintptr_t>(p.Y) & 15u) == 0 && p.ldy * (p.type == QVGGT_FP32 ? 4 : 2) % 16 == 0;
+    if (p.type == QVGGT_BF16) return tma ? launch_form<false, FORM_BF16>(c, st) : launch_form<false, ROWS_BF16>(c, st);
+    if (p.type == QVGGT_FP16) return tma ? launch_form<false, FORM_FP16>(c, st) : launch_form<false, ROWS_FP16>(c, st);
+    return tma ? launch_form<false, FORM_FP32>(c, st) : launch_form<false, ROWS_FP32>(c, st);
+}
+
+cudaError_t qvggt_read_linear_status(int *code) { return cudaMemcpyFromSymbol(code, linear_status, sizeof(int)); }

@@ -23,6 +23,8 @@ constexpr int RUN = 4;                                 // consecutive tiles of a
 constexpr int OPS_BYTES = 208 * 1024;                  // operands: [resident token rows,] ring of stages
 constexpr int MAX_STAGES = 12;
 
+__host__ __device__ __forceinline__ bool has_resident_rows(int K) { return (K + BK - 1) / BK == RES_KB; }
+
 // How the tiles are dealt to the workers; filled in by make_plan(), so that no thread of the kernel divides.  Work is counted in units of 256
 // token rows x 64 channels; whole tiles are numbered along the channels, row tile by row tile.
 struct Plan {
@@ -79,6 +81,14 @@ private:
     const Plan &p;
 };
 
+// Whether the plan's arithmetic holds for a product of this size: Plan::div() of a tile's number by the tiles of a row tile, and tile counts
+// in 32 bits.
+inline bool can_plan(int M, int N)
+{
+    const long long row_tiles = (M - 1LL) / (2 * BM) + 1, units = (N - 1LL) / UNIT + 1;
+    return row_tiles * units < (1LL << 31) && row_tiles * units < (1LL << 40) / units && row_tiles < (1LL << 24);
+}
+
 // Whole tiles first, as many as every worker gets alike, and what remains (less than a round of them) cut into pieces as narrow as one more
 // round allows: a launch of one round at K = 4096 takes 8.0 us with tiles of 64 channels, 8.2 - 8.7 with 128, 11.2 with 192 and 13.5 with 256
 // (K = 4096, N = 1024: 32.8 -> 29.9 us at 10 992 rows, 13.7 -> 11.2 at 2748; cut in halves only, or not at all, before).
@@ -100,15 +110,15 @@ private:
 // of the stores).
 inline Plan make_plan(int M, int N, int K, int max_workers, int *workers)
 {
-    const bool resident = K == RES_KB * BK;
+    const bool resident = has_resident_rows(K);
     Plan p = {};
     p.row_tiles = (M - 1) / (2 * BM) + 1;
-    p.NU = N / UNIT;
+    p.NU = (N - 1) / UNIT + 1;
     p.NT = (p.NU + MAX_UNITS - 1) / MAX_UNITS;
     // Where N is no multiple of 256, tiles of 128 channels may fit two rounds although those of up to 256 are just more than one, and two such
     // rounds cost less than one of 256 and one of 64 (layers, us, 256 + 64 / 128 + 128: K = 4096, N = 1152, 3867 rows 34.2 / 31.1, N = 640, 6500 rows
     // 42.3 / 39.0; K = 1024 11.55 / 11.16 and 12.95 / 12.55; three or more rounds: K = 1024, N = 1152, 8100 rows 17.35 / 17.7).
-    if (p.row_tiles * p.NT > max_workers && p.row_tiles * (p.NU / 2) <= 2 * max_workers) p.NT = p.NU / 2;
+    if (p.NU > 1 && p.row_tiles * p.NT > max_workers && p.row_tiles * (p.NU / 2) <= 2 * max_workers) p.NT = p.NU / 2;
     p.narrow = p.NU / p.NT;
     p.wider = p.NU % p.NT;
     p.wide = p.narrow + (p.wider ? 1 : 0);

@@ -135,3 +135,12 @@ cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st)
 {
     return p.type == QVGGT_BF16 ? by_rows<__nv_bfloat16>(p, st) : p.type == QVGGT_FP16 ? by_rows<__half>(p, st) : by_rows<float>(p, st);
 }
+
+cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st)
+{
+    if (p.M > 32) {
+        const cudaError_t e = qvggt_launch_linear_tiles(p, st);
+        if (e != cudaErrorNotSupported) return e;
+    }
+    return qvggt_launch_linear_few(p, st);
+}

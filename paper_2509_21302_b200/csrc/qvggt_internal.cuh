@@ -116,3 +116,6 @@ struct QvggtLinear {
     int M, N, K, type;
 };
 cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st);      // linear_few.cu
+cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st);    // gemm_c8.cu; cudaErrorNotSupported: sizes beyond its plan
+cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st);          // linear_few.cu: the one that suits the sizes
+cudaError_t qvggt_read_linear_status(int *code);                                 // the current device's status word of the launches without a handle

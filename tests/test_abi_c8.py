@@ -35,6 +35,7 @@ def test_missing_pointers():
             assert _norm(quant, **{name: None}) == NULL, name
     for name in ("Xq", "a", "Wq", "w", "Y"):
         assert _linear(**{name: None}) == NULL, name
+    assert q.lib().qvggt_linear_status(None, None) == NULL
 
 
 def test_sizes_and_strides():

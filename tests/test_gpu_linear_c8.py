@@ -8,6 +8,13 @@ from paper_2509_21302_b200 import binding
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True)
+def _no_wait_expired():
+    yield
+    assert q.linear_status() == 0
+
+
 U = 2.0 ** -24
 TYPES = [torch.bfloat16, torch.float16, torch.float32]
 
