@@ -472,6 +472,7 @@ int qvggt_linear_status(void *cuda_stream, int *code)
 {
     if (!code) return QVGGT_ERR_NULL;
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess || qvggt_read_linear_status(code) != cudaSuccess) return QVGGT_ERR_CUDA;
+    if (*code == 0 && qvggt_read_split_status(code) != cudaSuccess) return QVGGT_ERR_CUDA;
     return *code == 0 ? QVGGT_OK : QVGGT_ERR_DEVICE_TIMEOUT;
 }
 
