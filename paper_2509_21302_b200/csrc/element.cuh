@@ -42,32 +42,61 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     return w;
 }
 
-// Eight consecutive elements of a row.  `wide`: p is on a 16-byte boundary and all eight exist; otherwise the first n (0 .. 8) exist, the
-// others are read as zero and not written.
-template <class T>
-__device__ __forceinline__ void load8(const T *p, bool wide, int n, float (&v)[8])
-{
-    if (wide) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(p);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+// Eight consecutive elements of a row as they lie in memory: the 16-byte granules that hold them (a granule is read only where one of the n
+// elements, 1 .. 8, that exist lies in it).  fetch() only loads, so that many chunks can be on their way before the first is used.  With
+// WIDE every row begins on a 16-byte boundary; otherwise get() shifts the elements out of one granule more.
+template <class T, bool WIDE>
+struct Chunk {
+    static constexpr int SPAN = sizeof(T) / 2;                        // granules of eight elements
+    static constexpr int WORDS = 4 * (SPAN + (WIDE ? 0 : 1));
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2<T>(u[i]);
-                v[2 * i] = f.x;
-                v[2 * i + 1] = f.y;
-            }
-        } else {
-            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
     }
-}
+    __device__ __forceinline__ void fetch(const T *p, int n)
+    {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = WIDE ? at : at & ~uintptr_t(15), end = at + min(n, 8) * sizeof(T);
+#pragma unroll
+        for (int i = 0; i < WORDS / 4; ++i) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (i == 0 || base + 16 * i < end) v = *reinterpret_cast<const uint4 *>(base + 16 * i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+    }
+    // The values; those behind the first n are zero.
+    __device__ __forceinline__ void get(const T *p, int n, float (&v)[8]) const
+    {
+        uint32_t u[WORDS];
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) u[i] = w[i];
+        if constexpr (!WIDE) {
+            const uint32_t byte = reinterpret_cast<uintptr_t>(p) & 15;
+#pragma unroll
+            for (int i = 0; i + 2 < WORDS; ++i) u[i] = byte & 8 ? u[i + 2] : u[i];
+#pragma unroll
+            for (int i = 0; i + 1 < WORDS; ++i) u[i] = byte & 4 ? u[i + 1] : u[i];
+            if constexpr (sizeof(T) == 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = __funnelshift_r(u[i], u[i + 1], 8 * (byte & 2));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 2) {
+                const float2 f = unpack2<T>(u[i / 2]);
+                v[i] = i & 1 ? f.y : f.x;
+            } else {
+                v[i] = __uint_as_float(u[i]);
+            }
+        }
+        if (n < 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
+    }
+};
 
+// Stores eight elements: `wide`: p is on a 16-byte boundary and all eight exist; otherwise the first n of them, one by one.
 template <class T>
 __device__ __forceinline__ void store8(T *p, bool wide, int n, const float (&v)[8])
 {

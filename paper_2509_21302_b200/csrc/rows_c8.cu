@@ -15,7 +15,7 @@
 
 namespace {
 
-using element::load8;
+using element::Chunk;
 using element::store8;
 
 constexpr int WARP_ROWS = 8;               // rows of a CTA where a warp takes a row
@@ -30,7 +30,7 @@ struct Rows {
     long long ldx, ldr, ldh, ldy, ldq;     // in elements
     float eps;
     int M, K;
-    bool wide_x, wide_r, wide_h, wide_y, wide_q, wide_g;   // every row of it begins on a 16-byte boundary (q: 8 bytes)
+    bool wide_h, wide_y, wide_q;           // every row of it begins on a 16-byte boundary (q: 8 bytes)
 };
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -62,8 +62,8 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *part)
 }
 
 // A row's eight-element chunks t, t + threads, ... belong to thread t: CHUNKS of them in registers, or (CHUNKS = 0, rows too long for
-// that) any number, read again for every pass.
-template <class T, bool NORM, bool QUANT, bool WARP, int CHUNKS>
+// that) any number, read again for every pass.  WIDE: every row of x, r and gamma begins on a 16-byte boundary.
+template <class T, bool NORM, bool QUANT, bool WARP, bool WIDE, int CHUNKS>
 __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kernel(const __grid_constant__ Rows p)
 {
     __shared__ float part_sum[32];
@@ -77,26 +77,18 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kern
     const T *x = static_cast<const T *>(p.x) + m * p.ldx;
     const T *r = p.r ? static_cast<const T *>(p.r) + m * p.ldr : nullptr;
 
-    auto load = [&](int c, float (&v)[8]) {
-        const int k = 8 * c, n = p.K - k;
-        load8(x + k, p.wide_x && n >= 8, n, v);
-        if (NORM && r) {
-            float a[8];
-            load8(r + k, p.wide_r && n >= 8, n, a);
+    auto add = [](float (&v)[8], const float (&a)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += a[i];
-        }
+        for (int i = 0; i < 8; ++i) v[i] += a[i];
     };
     auto store_sum = [&](int c, const float (&v)[8]) {
         const int k = 8 * c, n = p.K - k;
         if (NORM && p.h) store8(static_cast<T *>(p.h) + m * p.ldh + k, p.wide_h && n >= 8, n, v);
     };
     float rstd = 1.0f;
-    auto normalize = [&](int c, float (&v)[8]) {
-        if (!NORM) return;
-        const int k = 8 * c, n = p.K - k;
+    auto normalize = [&](int c, const Chunk<float, WIDE> &gamma, float (&v)[8]) {
         float g[8];
-        load8(p.gamma + k, p.wide_g && n >= 8, n, g);
+        gamma.get(p.gamma + 8 * c, p.K - 8 * c, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (v[i] * rstd) * g[i];
     };
@@ -108,7 +100,7 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kern
             store8(static_cast<T *>(p.y) + m * p.ldy + k, p.wide_y && n >= 8, n, v);
         } else {
             uint32_t u[8];
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.0f));   // 1.5 * 2^23: the code is the low byte
             uint32_t lo = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
             uint32_t hi = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
@@ -117,7 +109,7 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kern
             if (p.wide_q && n >= 8) {
                 *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
             } else {
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (i < n) q[i] = static_cast<signed char>((i < 4 ? lo : hi) >> (8 * (i & 3)));
             }
@@ -144,24 +136,55 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kern
     };
 
     if constexpr (CHUNKS > 0) {
+        // Everything that is read is on its way before the first value is used (a chunk at a time, with the choice of wide and narrow
+        // loads in between, each load waited for the one before it: 43 968 x 4096 bf16, norm and codes 185 us).
+        Chunk<T, WIDE> cx[CHUNKS], cr[CHUNKS];
+        Chunk<float, WIDE> cg[CHUNKS];
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int c = t + i * threads;
+            cx[i].clear();
+            if (c < chunks) cx[i].fetch(x + 8 * c, p.K - 8 * c);
+        }
+        if (NORM && r) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int c = t + i * threads;
+                cr[i].clear();
+                if (c < chunks) cr[i].fetch(r + 8 * c, p.K - 8 * c);
+            }
+        }
+        if (NORM) {
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int c = t + i * threads;
+                cg[i].clear();
+                if (c < chunks) cg[i].fetch(p.gamma + 8 * c, p.K - 8 * c);
+            }
+        }
         float v[CHUNKS][8];
 #pragma unroll
-        for (int i = 0; i < CHUNKS; ++i)
-            if (t + i * threads < chunks) load(t + i * threads, v[i]);
-            else
+        for (int i = 0; i < CHUNKS; ++i) cx[i].get(x + 8 * (t + i * threads), p.K - 8 * (t + i * threads), v[i]);
+        if (NORM && r) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            for (int i = 0; i < CHUNKS; ++i) {
+                float a[8];
+                cr[i].get(r + 8 * (t + i * threads), p.K - 8 * (t + i * threads), a);
+                add(v[i], a);
+            }
+        }
         if (NORM) {
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                if (t + i * threads < chunks) store_sum(t + i * threads, v[i]);
-                s += square(v[i]);
+            for (int i = 0; i < CHUNKS; ++i) s += square(v[i]);
+            if (p.h) {
+#pragma unroll
+                for (int i = 0; i < CHUNKS; ++i)
+                    if (t + i * threads < chunks) store_sum(t + i * threads, v[i]);
             }
             finish_sum(s);
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i)
-                if (t + i * threads < chunks) normalize(t + i * threads, v[i]);
+            for (int i = 0; i < CHUNKS; ++i) normalize(t + i * threads, cg[i], v[i]);
         }
         if (QUANT) {
             uint32_t a = 0;
@@ -174,42 +197,76 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kern
             if (t + i * threads < chunks) store_row(t + i * threads, v[i]);
     } else {
         float v[8];
+        auto load = [&](int c) {
+            const int n = p.K - 8 * c;
+            Chunk<T, WIDE> cx, cr;
+            cx.fetch(x + 8 * c, n);
+            if (NORM && r) cr.fetch(r + 8 * c, n);
+            cx.get(x + 8 * c, n, v);
+            if (NORM && r) {
+                float a[8];
+                cr.get(r + 8 * c, n, a);
+                add(v, a);
+            }
+        };
+        auto normalized = [&](int c) {
+            if (!NORM) return;
+            Chunk<float, WIDE> cg;
+            cg.fetch(p.gamma + 8 * c, p.K - 8 * c);
+            normalize(c, cg, v);
+        };
         if (NORM) {
             float s = 0.0f;
-            for (int c = t; c < chunks; c += threads) { load(c, v); s += square(v); }
+            for (int c = t; c < chunks; c += threads) { load(c); s += square(v); }
             finish_sum(s);
         }
         if (QUANT) {
             uint32_t a = 0;
-            for (int c = t; c < chunks; c += threads) { load(c, v); normalize(c, v); a = largest(v, a); }
+            for (int c = t; c < chunks; c += threads) { load(c); normalized(c); a = largest(v, a); }
             finish_max(a);
         }
         // the sum is stored last: it may take the place of x or r, which every pass reads
-        for (int c = t; c < chunks; c += threads) { load(c, v); store_sum(c, v); normalize(c, v); store_row(c, v); }
+        for (int c = t; c < chunks; c += threads) { load(c); store_sum(c, v); normalized(c); store_row(c, v); }
     }
 }
 
-// v = q * scale, eight codes per thread.
+// v = q * scale, eight codes per thread, DEQ_ROWS rows of them at once.  A CTA is `columns` threads wide along a row, 256 / columns rows high.
+constexpr int DEQ_ROWS = 4;
 template <class T>
-__global__ void __launch_bounds__(256) dequantize_kernel(const signed char *q, long long ldq, const float *scales, T *y, long long ldy, int M, int K, bool wide_q, bool wide_y)
+__global__ void __launch_bounds__(256) dequantize_kernel(const signed char *q, long long ldq, const float *scales, T *y, long long ldy, int M, int K, int columns, bool wide_q, bool wide_y)
 {
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const long long m = blockIdx.y + (long long)gridDim.y * blockIdx.z;
-    const int c = blockIdx.x * 256 + threadIdx.x, k = 8 * c, n = K - k;
-    if (m >= M || n <= 0) return;
-    const signed char *src = q + m * ldq + k;
-    const float s = scales[m];
-    float v[8];
-    if (wide_q && n >= 8) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(src);
+    const int high = 256 / columns, row = threadIdx.x / columns;
+    const int k = 8 * (blockIdx.y * columns + threadIdx.x % columns), n = K - k;
+    const long long m0 = (long long)blockIdx.x * (high * DEQ_ROWS) + row;
+    if (row >= high || n <= 0) return;
+    uint2 w[DEQ_ROWS];
+    float s[DEQ_ROWS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(static_cast<signed char>((i < 4 ? w.x : w.y) >> (8 * (i & 3)))) * s;
-    } else {
+    for (int i = 0; i < DEQ_ROWS; ++i) {
+        const long long m = m0 + i * high;
+        w[i] = make_uint2(0, 0);
+        s[i] = 0.0f;
+        if (m < M) {
+            const signed char *src = q + m * ldq + k;
+            s[i] = scales[m];
+            if (wide_q && n >= 8) w[i] = *reinterpret_cast<const uint2 *>(src);
+            else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? static_cast<float>(src[i]) * s : 0.0f;
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) (j < 4 ? w[i].x : w[i].y) |= static_cast<uint32_t>(static_cast<unsigned char>(src[j])) << (8 * (j & 3));
+        }
     }
-    store8(y + m * ldy + k, wide_y && n >= 8, n, v);
+#pragma unroll
+    for (int i = 0; i < DEQ_ROWS; ++i) {
+        const long long m = m0 + i * high;
+        if (m >= M) continue;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<signed char>((j < 4 ? w[i].x : w[i].y) >> (8 * (j & 3)))) * s[i];
+        store8(y + m * ldy + k, wide_y && n >= 8, n, v);
+    }
 }
 
 template <class Kernel, class... Args>
@@ -227,24 +284,25 @@ cudaError_t launch(Kernel kernel, dim3 grid, int threads, cudaStream_t st, Args.
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <class T, bool NORM, bool QUANT>
+template <class T, bool NORM, bool QUANT, bool WIDE>
 cudaError_t dispatch(const Rows &p, cudaStream_t st)
 {
     const int chunks = (p.K + 7) / 8;
-    if (chunks <= 128) {
+    if (chunks <= 64) {
         const dim3 grid((p.M - 1) / WARP_ROWS + 1);
-        if (chunks <= 32) return launch(rows_kernel<T, NORM, QUANT, true, 1>, grid, WARP_ROWS * 32, st, p);
-        if (chunks <= 64) return launch(rows_kernel<T, NORM, QUANT, true, 2>, grid, WARP_ROWS * 32, st, p);
-        return launch(rows_kernel<T, NORM, QUANT, true, 4>, grid, WARP_ROWS * 32, st, p);
+        if (chunks <= 32) return launch(rows_kernel<T, NORM, QUANT, true, WIDE, 1>, grid, WARP_ROWS * 32, st, p);
+        return launch(rows_kernel<T, NORM, QUANT, true, WIDE, 2>, grid, WARP_ROWS * 32, st, p);
     }
-    if (chunks <= 4 * MAX_THREADS) return launch(rows_kernel<T, NORM, QUANT, false, 4>, dim3(p.M), (chunks + 127) / 128 * 32, st, p);
-    return launch(rows_kernel<T, NORM, QUANT, false, 0>, dim3(p.M), MAX_THREADS, st, p);
+    if (chunks <= 2 * MAX_THREADS) return launch(rows_kernel<T, NORM, QUANT, false, WIDE, 2>, dim3(p.M), (chunks + 63) / 64 * 32, st, p);
+    return launch(rows_kernel<T, NORM, QUANT, false, WIDE, 0>, dim3(p.M), MAX_THREADS, st, p);
 }
 
 template <bool NORM, bool QUANT>
-cudaError_t by_type(int type, const Rows &p, cudaStream_t st)
+cudaError_t by_type(int type, bool wide, const Rows &p, cudaStream_t st)
 {
-    return type == QVGGT_BF16 ? dispatch<__nv_bfloat16, NORM, QUANT>(p, st) : type == QVGGT_FP16 ? dispatch<__half, NORM, QUANT>(p, st) : dispatch<float, NORM, QUANT>(p, st);
+    if (type == QVGGT_BF16) return wide ? dispatch<__nv_bfloat16, NORM, QUANT, true>(p, st) : dispatch<__nv_bfloat16, NORM, QUANT, false>(p, st);
+    if (type == QVGGT_FP16) return wide ? dispatch<__half, NORM, QUANT, true>(p, st) : dispatch<__half, NORM, QUANT, false>(p, st);
+    return wide ? dispatch<float, NORM, QUANT, true>(p, st) : dispatch<float, NORM, QUANT, false>(p, st);
 }
 
 int bytes_of(int type) { return type == QVGGT_FP32 ? 4 : 2; }
@@ -264,22 +322,20 @@ cudaError_t qvggt_launch_rows(int type, const void *X, long long ldx, const void
     p.x = X; p.r = R; p.h = H; p.y = Y; p.q = Xq8; p.scales = scales; p.gamma = gamma;
     p.ldx = ldx; p.ldr = ldr; p.ldh = ldh; p.ldy = ldy; p.ldq = ldq;
     p.eps = eps; p.M = M; p.K = K;
-    p.wide_x = rows_aligned(X, ldx, e, 16);
-    p.wide_r = rows_aligned(R, ldr, e, 16);
+    const bool wide = rows_aligned(X, ldx, e, 16) && (!R || rows_aligned(R, ldr, e, 16)) && rows_aligned(gamma, 0, 4, 16);
     p.wide_h = rows_aligned(H, ldh, e, 16);
     p.wide_y = rows_aligned(Y, ldy, e, 16);
     p.wide_q = rows_aligned(Xq8, ldq, 1, 8);
-    p.wide_g = rows_aligned(gamma, 0, 4, 16);
-    if (!gamma) return by_type<false, true>(type, p, st);
-    return Xq8 ? by_type<true, true>(type, p, st) : by_type<true, false>(type, p, st);
+    if (!gamma) return by_type<false, true>(type, wide, p, st);
+    return Xq8 ? by_type<true, true>(type, wide, p, st) : by_type<true, false>(type, wide, p, st);
 }
 
 cudaError_t qvggt_launch_dequantize(int type, const signed char *Xq8, long long ldq, const float *scales, int M, int K, void *Y, long long ldy, cudaStream_t st)
 {
     const bool wide_q = rows_aligned(Xq8, ldq, 1, 8), wide_y = rows_aligned(Y, ldy, bytes_of(type), 16);
-    const unsigned gy = M < 32768 ? M : 32768;
-    const dim3 grid((K + 2047) / 2048, gy, (M - 1) / gy + 1);
-    if (type == QVGGT_BF16) return launch(dequantize_kernel<__nv_bfloat16>, grid, 256, st, Xq8, ldq, scales, static_cast<__nv_bfloat16 *>(Y), ldy, M, K, wide_q, wide_y);
-    if (type == QVGGT_FP16) return launch(dequantize_kernel<__half>, grid, 256, st, Xq8, ldq, scales, static_cast<__half *>(Y), ldy, M, K, wide_q, wide_y);
-    return launch(dequantize_kernel<float>, grid, 256, st, Xq8, ldq, scales, static_cast<float *>(Y), ldy, M, K, wide_q, wide_y);
+    const int chunks = (K + 7) / 8, wide = (chunks + 255) / 256, columns = (chunks + wide - 1) / wide, high = 256 / columns * DEQ_ROWS;
+    const dim3 grid((M - 1) / high + 1, wide);
+    if (type == QVGGT_BF16) return launch(dequantize_kernel<__nv_bfloat16>, grid, 256, st, Xq8, ldq, scales, static_cast<__nv_bfloat16 *>(Y), ldy, M, K, columns, wide_q, wide_y);
+    if (type == QVGGT_FP16) return launch(dequantize_kernel<__half>, grid, 256, st, Xq8, ldq, scales, static_cast<__half *>(Y), ldy, M, K, columns, wide_q, wide_y);
+    return launch(dequantize_kernel<float>, grid, 256, st, Xq8, ldq, scales, static_cast<float *>(Y), ldy, M, K, columns, wide_q, wide_y);
 }
