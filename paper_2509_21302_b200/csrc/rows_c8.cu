@@ -3,20 +3,24 @@
 //   h[k] = x[k] + r[k]                             (stored, if asked for, rounded to the type; what follows uses the unrounded sum)
 //   y[k] = (h[k] * rstd) * gamma[k],  rstd = 1 / sqrt(sum h^2 / K + eps)
 //   amax = max(max_k |y[k]|, 1e-8),  scale = amax / 127,  q[k] = round(y[k] * (127 * (1 / amax))), half to even
-// Every one of these operations is rounded to fp32 by itself, so that the codes of given y are those of the formula in plain fp32 arithmetic,
-// bit for bit.  That shows where elements of 16 bits lie exactly between two codes: with the product rounded straight to the integer (one
-// multiply-add) other codes came out there.
+// In the quantizer every one of these operations is rounded to fp32 by itself, so that its codes are those of the formula in plain fp32
+// arithmetic, bit for bit.  That shows where elements of 16 bits lie exactly between two codes: with the product rounded straight to the
+// integer (one multiply-add) other codes came out there.
 // They move K e bytes in, K (and K e) out, against a handful of operations per element: HBM bounds them from a few hundred rows on,
 // and latency (one load, two reductions, one store) below.  A row therefore stays in registers between its one load and its one store.
 #include "element.cuh"
+#include "gemm_common.cuh"
 #include "qvggt_internal.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
 
 namespace {
 
+using element::ANY;
 using element::Chunk;
+using element::REGULAR;
 using element::store8;
+using element::store16;
 
 constexpr int WARP_ROWS = 8;               // rows of a CTA where a warp takes a row
 constexpr int MAX_THREADS = 1024;
@@ -28,249 +32,325 @@ struct Rows {
     float *scales;
     const float *gamma;
     long long ldx, ldr, ldh, ldy, ldq;     // in elements
-    float eps;
+    float eps, one_over_k, floor_factor;   // floor_factor: 127 * (1 / 1e-8), every operation rounded
     int M, K;
+    uint32_t zero;                         // 0, which the compiler cannot know (ptx::f32x2_one)
     bool wide_h, wide_y, wide_q;           // every row of it begins on a 16-byte boundary (q: 8 bytes)
 };
 
-__device__ __forceinline__ float warp_sum(float v)
+// Sum of s and largest of a over `lanes` neighbouring lanes (a power of two).
+template <bool SUM, bool MAX>
+__device__ __forceinline__ void reduce_lanes(float &s, uint32_t &a, int lanes)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    return v;
+    for (int o = 16; o; o >>= 1)
+        if (SUM && o < lanes) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (MAX) a = __reduce_max_sync(0xFFFFFFFFu, a);
 }
 
-// Sum / largest of a value per thread over the row's threads: a warp, or the CTA (every thread gets the result; `part` holds 32 words).
-template <bool WARP>
-__device__ __forceinline__ float row_sum(float v, float *part)
+// The same over the row's threads: a warp, or the CTA, which meets once for both (every thread gets the results; `part` holds 32 pairs that
+// no thread still reads from an earlier call: two meetings back is enough).
+template <bool WARP, bool SUM, bool MAX>
+__device__ __forceinline__ void reduce_row(float &s, uint32_t &a, uint2 *part)
 {
-    v = warp_sum(v);
-    if (WARP) return v;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    reduce_lanes<SUM, MAX>(s, a, 32);
+    if (WARP) return;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    if (lane == 0) part[threadIdx.x >> 5] = make_uint2(__float_as_uint(s), a);
     __syncthreads();
-    return warp_sum((threadIdx.x & 31) < (blockDim.x >> 5) ? part[threadIdx.x & 31] : 0.0f);
+    const int lanes = warps <= 4 ? 4 : warps <= 8 ? 8 : 32, mine = lane & (lanes - 1);
+    const uint2 v = mine < warps ? part[mine] : make_uint2(0, 0);
+    s = __uint_as_float(v.x);
+    a = v.y;
+    reduce_lanes<SUM, MAX>(s, a, lanes);
 }
 
-template <bool WARP>
-__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *part)
+// The arithmetic on a row's chunks of eight elements, two elements in a word; the same in both kernels below.
+// With both, norm and codes, the values that go into the quantizer are w = h gamma: rstd is common to all of a row, so the codes of
+// y = rstd w are those of w, and sum and maximum are taken in one pass (two passes with a meeting each: 43 968 x 4096 bf16 172 us).
+template <class T, bool NORM, bool QUANT, int LAYOUT>
+struct Row {
+    float sum = 0.0f;
+    uint32_t top = 0;                                    // bits of the largest magnitude: NaN is the largest of all
+    uint64_t factor = 0;                                 // rstd, or what turns values into codes
+    bool finite = true;
+
+    // Takes values into sum and maximum; with codes behind the norm, v turns into w.
+    __device__ __forceinline__ void take(uint64_t (&v)[4], const uint64_t (&g)[4])
+    {
+        if (NORM) {
+            uint64_t s = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = ptx::f32x2_fma(v[i], v[i], s);
+            float lo, hi;
+            ptx::f32x2_unpack(s, lo, hi);
+            sum += lo + hi;
+        }
+        if (QUANT) {
+            float t = __uint_as_float(top);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (NORM) v[i] = ptx::f32x2_mul(v[i], g[i]);
+                float lo, hi;
+                ptx::f32x2_unpack(v[i], lo, hi);
+                asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(t) : "f"(t), "f"(lo), "f"(hi));
+            }
+            top = __float_as_uint(t);
+        }
+    }
+    // scale: where the row's goes, in one of its threads.
+    __device__ __forceinline__ void end(const Rows &p, float *scale)
+    {
+        float rstd = 1.0f;
+        if (NORM) rstd = rsqrtf(__fmaf_rn(sum, p.one_over_k, p.eps));
+        if (QUANT) {
+            const float t = __uint_as_float(top), amax = NORM ? __fmul_rn(t, rstd) : t;
+            finite = top < 0x7F800000u && !(amax != amax);
+            const float f = amax >= 1e-8f ? __fmul_rn(__frcp_rn(t), 127.0f) : __fmul_rn(p.floor_factor, rstd);
+            factor = ptx::f32x2_pack(f, f);
+            if (scale) *scale = finite ? __fdiv_rn(fmaxf(amax, 1e-8f), 127.0f) : __uint_as_float(0x7FC00000u);
+        } else {
+            factor = ptx::f32x2_pack(rstd, rstd);
+        }
+    }
+    // Results of a chunk, n elements from its first on, to y.
+    __device__ __forceinline__ void store(T *y, bool wide, int n, const uint64_t (&v)[4], const uint64_t (&g)[4]) const
+    {
+        uint64_t z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = ptx::f32x2_mul(ptx::f32x2_mul(v[i], factor), g[i]);
+        store8(y, LAYOUT == REGULAR || (wide && n >= 8), n, z);
+    }
+    __device__ __forceinline__ void store(signed char *q, bool wide, int n, const uint64_t (&v)[4], uint64_t one2) const
+    {
+        const uint64_t magic = ptx::f32x2_pack(12582912.0f, 12582912.0f);            // 1.5 * 2^23: the code is the low byte
+        uint32_t u[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            ptx::f32x2_unpack(ptx::f32x2_add_uncontracted(ptx::f32x2_mul(v[i], factor), magic, one2), lo, hi);
+            u[2 * i] = __float_as_uint(lo);
+            u[2 * i + 1] = __float_as_uint(hi);
+        }
+        uint32_t lo = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+        uint32_t hi = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
+        lo = finite ? lo : 0;
+        hi = finite ? hi : 0;
+        if (LAYOUT == REGULAR || (wide && n >= 8)) {
+            *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) q[i] = static_cast<signed char>((i < 4 ? lo : hi) >> (8 * (i & 3)));
+        }
+    }
+};
+
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void async_wait(int pending)       // at most so many groups (0 or 1) still on their way
 {
-    v = __reduce_max_sync(0xFFFFFFFFu, v);
-    if (WARP) return v;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return __reduce_max_sync(0xFFFFFFFFu, (threadIdx.x & 31) < (blockDim.x >> 5) ? part[threadIdx.x & 31] : 0u);
+    if (pending <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;" ::: "memory");
 }
 
-// A row's eight-element chunks t, t + threads, ... belong to thread t: CHUNKS of them in registers, or (CHUNKS = 0, rows too long for
-// that) any number, read again for every pass.  WIDE: every row of x, r and gamma begins on a 16-byte boundary.
-template <class T, bool NORM, bool QUANT, bool WARP, bool WIDE, int CHUNKS>
-__global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS) rows_kernel(const __grid_constant__ Rows p)
+// Rows in registers: thread t of a row's threads (a warp, or the CTA) has the chunks t, t + threads, .. (CHUNKS of them).  A warp or CTA
+// takes `turns` rows; while one is worked on, the next `depth` are on their way to shared memory, each warp fetching what it will read
+// itself, so that no warp waits for another but in the reduction.  gamma stays in registers.
+template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
+__global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (CHUNKS > 1 ? 3 : 4) : 1) rows_kernel(const __grid_constant__ Rows p, int turns, int depth)
 {
-    __shared__ float part_sum[32];
-    __shared__ uint32_t part_max[32];
+    using C = Chunk<T, LAYOUT>;
+    constexpr uint32_t BLOCK = C::WARP_GRANULES * 16, TENSOR = CHUNKS * BLOCK;
+    extern __shared__ uint4 ring[];                                          // [warp][depth][x, r][CHUNKS][granules]
+    __shared__ uint2 part[2][32];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const long long m = WARP ? (long long)blockIdx.x * WARP_ROWS + (threadIdx.x >> 5) : blockIdx.x;
-    if (m >= p.M) return;                                                    // (whole warps)
-    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x;
-    const int chunks = (p.K + 7) / 8;
-    const T *x = static_cast<const T *>(p.x) + m * p.ldx;
-    const T *r = p.r ? static_cast<const T *>(p.r) + m * p.ldr : nullptr;
+    constexpr int step = WARP ? WARP_ROWS : 1;
+    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x, lane = threadIdx.x & 31;
+    const bool residual = NORM && p.r;
+    const uint32_t slot_bytes = residual ? 2 * TENSOR : TENSOR, mine = ptx::smem_addr(ring) + (threadIdx.x >> 5) * depth * slot_bytes;
+    const long long m0 = (long long)blockIdx.x * turns * step + (WARP ? threadIdx.x >> 5 : 0), left = (p.M - m0 + step - 1) / step;
+    const int rows = left < turns ? (int)left : turns;                       // of this warp or CTA
+    int at[CHUNKS], n[CHUNKS];                                               // a chunk's first element, elements from there on
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+        at[i] = 8 * (t + i * threads);
+        n[i] = p.K - at[i];
+    }
+    // rows of this thread's, one after the other: read, fetched ahead, written
+    const T *x = static_cast<const T *>(p.x) + m0 * p.ldx, *r = static_cast<const T *>(p.r) + m0 * p.ldr, *x_ahead = x, *r_ahead = r;
+    T *h = static_cast<T *>(p.h) + m0 * p.ldh, *y = static_cast<T *>(p.y) + m0 * p.ldy;
+    signed char *q = p.q + m0 * p.ldq;
+    float *scale = QUANT && t == 0 ? p.scales + m0 : nullptr;
+    const uint64_t one2 = ptx::f32x2_one(p.zero);
 
-    auto add = [](float (&v)[8], const float (&a)[8]) {
+    auto fetch = [&](int turn, uint32_t slot) {
+        if (turn < rows) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += a[i];
-    };
-    auto store_sum = [&](int c, const float (&v)[8]) {
-        const int k = 8 * c, n = p.K - k;
-        if (NORM && p.h) store8(static_cast<T *>(p.h) + m * p.ldh + k, p.wide_h && n >= 8, n, v);
-    };
-    float rstd = 1.0f;
-    auto normalize = [&](int c, const Chunk<float, WIDE> &gamma, float (&v)[8]) {
-        float g[8];
-        gamma.get(p.gamma + 8 * c, p.K - 8 * c, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (v[i] * rstd) * g[i];
-    };
-    float inv = 0.0f;
-    bool finite = true;
-    auto store_row = [&](int c, const float (&v)[8]) {
-        const int k = 8 * c, n = p.K - k;
-        if constexpr (!QUANT) {
-            store8(static_cast<T *>(p.y) + m * p.ldy + k, p.wide_y && n >= 8, n, v);
-        } else {
-            uint32_t u[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.0f));   // 1.5 * 2^23: the code is the low byte
-            uint32_t lo = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
-            uint32_t hi = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
-            if (!finite) lo = hi = 0;
-            signed char *q = p.q + m * p.ldq + k;
-            if (p.wide_q && n >= 8) {
-                *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n) q[i] = static_cast<signed char>((i < 4 ? lo : hi) >> (8 * (i & 3)));
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int a = at[i] - 8 * lane;                              // the warp's first
+                C::fetch_async(slot + i * BLOCK, x_ahead + a, p.K - a, lane);
+                if (residual) C::fetch_async(slot + TENSOR + i * BLOCK, r_ahead + a, p.K - a, lane);
             }
+            x_ahead += step * p.ldx;
+            r_ahead += step * p.ldr;
         }
+        async_commit();
     };
-    auto square = [](const float (&v)[8]) {
-        float s = 0.0f;
+    for (int d = 0; d < depth; ++d) fetch(d, mine + d * slot_bytes);
+    uint64_t g[CHUNKS][4] = {};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = __fmaf_rn(v[i], v[i], s);
-        return s;
-    };
-    auto largest = [](const float (&v)[8], uint32_t a) {                     // on the bits: NaN is the largest of all
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-        return a;
-    };
-    auto finish_sum = [&](float s) { rstd = __frsqrt_rn(__fdiv_rn(row_sum<WARP>(s, part_sum), (float)p.K) + p.eps); };
-    auto finish_max = [&](uint32_t a) {
-        a = row_max<WARP>(a, part_max);
-        finite = a < 0x7F800000u;
-        const float amax = fmaxf(__uint_as_float(a), 1e-8f);
-        inv = __fmul_rn(__frcp_rn(amax), 127.0f);
-        if (t == 0) p.scales[m] = finite ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
-    };
-
-    if constexpr (CHUNKS > 0) {
-        // Everything that is read is on its way before the first value is used (a chunk at a time, with the choice of wide and narrow
-        // loads in between, each load waited for the one before it: 43 968 x 4096 bf16, norm and codes 185 us).
-        Chunk<T, WIDE> cx[CHUNKS], cr[CHUNKS];
-        Chunk<float, WIDE> cg[CHUNKS];
+    for (int i = 0; i < CHUNKS; ++i)
+        if (NORM && n[i] > 0) {
+            Chunk<float, LAYOUT> c;
+            c.fetch(p.gamma + at[i], n[i]);
+            c.get(p.gamma + at[i], n[i], g[i]);
+        }
+    uint32_t slot = mine;
+    for (int turn = 0; turn < rows; ++turn) {
+        Row<T, NORM, QUANT, LAYOUT> row;
+        uint64_t v[CHUNKS][4];
+        async_wait(depth - 1);
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i) {
-            const int c = t + i * threads;
-            cx[i].clear();
-            if (c < chunks) cx[i].fetch(x + 8 * c, p.K - 8 * c);
-        }
-        if (NORM && r) {
+            C c;
+            c.fetched(slot + i * BLOCK, lane);
+            c.get(x + at[i], n[i], v[i]);
+            if (residual) {
+                uint64_t a[4];
+                c.fetched(slot + TENSOR + i * BLOCK, lane);
+                c.get(r + at[i], n[i], a);
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const int c = t + i * threads;
-                cr[i].clear();
-                if (c < chunks) cr[i].fetch(r + 8 * c, p.K - 8 * c);
+                for (int j = 0; j < 4; ++j) v[i][j] = ptx::f32x2_add(v[i][j], a[j]);
             }
+            if (LAYOUT == REGULAR && n[i] <= 0)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = 0;
         }
-        if (NORM) {
+        __syncwarp();                                                        // every lane has read the slot that is fetched into now
+        fetch(turn + depth, slot);
+        slot = slot == mine && depth > 1 ? mine + slot_bytes : mine;
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                const int c = t + i * threads;
-                cg[i].clear();
-                if (c < chunks) cg[i].fetch(p.gamma + 8 * c, p.K - 8 * c);
-            }
+        for (int i = 0; i < CHUNKS; ++i) {
+            if (NORM && p.h && n[i] > 0) store8(h + at[i], LAYOUT == REGULAR || (p.wide_h && n[i] >= 8), n[i], v[i]);
+            row.take(v[i], g[i]);
         }
-        float v[CHUNKS][8];
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) cx[i].get(x + 8 * (t + i * threads), p.K - 8 * (t + i * threads), v[i]);
-        if (NORM && r) {
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
-                float a[8];
-                cr[i].get(r + 8 * (t + i * threads), p.K - 8 * (t + i * threads), a);
-                add(v[i], a);
-            }
-        }
-        if (NORM) {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) s += square(v[i]);
-            if (p.h) {
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i)
-                    if (t + i * threads < chunks) store_sum(t + i * threads, v[i]);
-            }
-            finish_sum(s);
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) normalize(t + i * threads, cg[i], v[i]);
-        }
-        if (QUANT) {
-            uint32_t a = 0;
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) a = largest(v[i], a);
-            finish_max(a);
-        }
+        reduce_row<WARP, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
+        row.end(p, scale);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
-            if (t + i * threads < chunks) store_row(t + i * threads, v[i]);
-    } else {
-        float v[8];
-        auto load = [&](int c) {
-            const int n = p.K - 8 * c;
-            Chunk<T, WIDE> cx, cr;
-            cx.fetch(x + 8 * c, n);
-            if (NORM && r) cr.fetch(r + 8 * c, n);
-            cx.get(x + 8 * c, n, v);
-            if (NORM && r) {
-                float a[8];
-                cr.get(r + 8 * c, n, a);
-                add(v, a);
+            if (n[i] > 0) {
+                if constexpr (QUANT) row.store(q + at[i], p.wide_q, n[i], v[i], one2);
+                else row.store(y + at[i], p.wide_y, n[i], v[i], g[i]);
             }
-        };
-        auto normalized = [&](int c) {
-            if (!NORM) return;
-            Chunk<float, WIDE> cg;
-            cg.fetch(p.gamma + 8 * c, p.K - 8 * c);
-            normalize(c, cg, v);
-        };
-        if (NORM) {
-            float s = 0.0f;
-            for (int c = t; c < chunks; c += threads) { load(c); s += square(v); }
-            finish_sum(s);
-        }
-        if (QUANT) {
-            uint32_t a = 0;
-            for (int c = t; c < chunks; c += threads) { load(c); normalized(c); a = largest(v, a); }
-            finish_max(a);
-        }
-        // the sum is stored last: it may take the place of x or r, which every pass reads
-        for (int c = t; c < chunks; c += threads) { load(c); store_sum(c, v); normalized(c); store_row(c, v); }
+        if (LAYOUT == ANY) { x += step * p.ldx; r += step * p.ldr; }         // (only where the row begins in its granule is asked of them)
+        if (NORM) h += step * p.ldh;
+        if (QUANT) { q += step * p.ldq; scale = scale ? scale + step : scale; }
+        else y += step * p.ldy;
     }
 }
 
-// v = q * scale, eight codes per thread, DEQ_ROWS rows of them at once.  A CTA is `columns` threads wide along a row, 256 / columns rows high.
+// Rows too long for that: a CTA reads its row twice.
+template <class T, bool NORM, bool QUANT, int LAYOUT>
+__global__ void __launch_bounds__(MAX_THREADS) long_rows_kernel(const __grid_constant__ Rows p)
+{
+    __shared__ uint2 part[32];
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    const long long m = blockIdx.x;
+    const T *x = static_cast<const T *>(p.x) + m * p.ldx, *r = static_cast<const T *>(p.r) + m * p.ldr;
+    const bool residual = NORM && p.r;
+    Row<T, NORM, QUANT, LAYOUT> row;
+    uint64_t v[4], g[4];
+    auto load = [&](int at) {
+        const int n = p.K - at;
+        Chunk<T, LAYOUT> cx, cr;
+        Chunk<float, LAYOUT> cg;
+        cx.fetch(x + at, n);
+        if (residual) cr.fetch(r + at, n);
+        if (NORM) cg.fetch(p.gamma + at, n);
+        cx.get(x + at, n, v);
+        if (residual) {
+            uint64_t a[4];
+            cr.get(r + at, n, a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = ptx::f32x2_add(v[i], a[i]);
+        }
+        if (NORM) cg.get(p.gamma + at, n, g);
+    };
+    for (int at = 8 * threadIdx.x; at < p.K; at += 8 * MAX_THREADS) { load(at); row.take(v, g); }
+    reduce_row<false, NORM, QUANT>(row.sum, row.top, part);
+    row.end(p, QUANT && threadIdx.x == 0 ? p.scales + m : nullptr);
+    const uint64_t one2 = ptx::f32x2_one(p.zero);
+    // the sum is stored in the last pass: it may take the place of x or r, which both read
+    for (int at = 8 * threadIdx.x; at < p.K; at += 8 * MAX_THREADS) {
+        const int n = p.K - at;
+        load(at);
+        if (NORM && p.h) store8(static_cast<T *>(p.h) + m * p.ldh + at, LAYOUT == REGULAR || (p.wide_h && n >= 8), n, v);
+        if constexpr (QUANT) {
+            if (NORM)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = ptx::f32x2_mul(v[i], g[i]);
+            row.store(p.q + m * p.ldq + at, p.wide_q, n, v, one2);
+        } else {
+            row.store(static_cast<T *>(p.y) + m * p.ldy + at, p.wide_y, n, v, g);
+        }
+    }
+}
+
+// v = q * scale: 16 bytes of results per thread, DEQ_ROWS rows of them at once.  A CTA is `columns` threads wide along a row, 256 / columns
+// rows high.
 constexpr int DEQ_ROWS = 4;
 template <class T>
 __global__ void __launch_bounds__(256) dequantize_kernel(const signed char *q, long long ldq, const float *scales, T *y, long long ldy, int M, int K, int columns, bool wide_q, bool wide_y)
 {
+    constexpr int E = 16 / sizeof(T);
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int high = 256 / columns, row = threadIdx.x / columns;
-    const int k = 8 * (blockIdx.y * columns + threadIdx.x % columns), n = K - k;
+    const int k = E * (blockIdx.y * columns + threadIdx.x % columns), n = K - k;
     const long long m0 = (long long)blockIdx.x * (high * DEQ_ROWS) + row;
     if (row >= high || n <= 0) return;
-    uint2 w[DEQ_ROWS];
+    uint32_t w[DEQ_ROWS][E / 4];
     float s[DEQ_ROWS];
 #pragma unroll
     for (int i = 0; i < DEQ_ROWS; ++i) {
         const long long m = m0 + i * high;
-        w[i] = make_uint2(0, 0);
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j) w[i][j] = 0;
         s[i] = 0.0f;
         if (m < M) {
             const signed char *src = q + m * ldq + k;
             s[i] = scales[m];
-            if (wide_q && n >= 8) w[i] = *reinterpret_cast<const uint2 *>(src);
-            else
+            if (wide_q && n >= E) {
+                if constexpr (E == 8) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(src);
+                    w[i][0] = u.x;
+                    w[i][1] = u.y;
+                } else {
+                    w[i][0] = *reinterpret_cast<const uint32_t *>(src);
+                }
+            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < n) (j < 4 ? w[i].x : w[i].y) |= static_cast<uint32_t>(static_cast<unsigned char>(src[j])) << (8 * (j & 3));
+                for (int j = 0; j < E; ++j)
+                    if (j < n) w[i][j / 4] |= static_cast<uint32_t>(static_cast<unsigned char>(src[j])) << (8 * (j & 3));
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < DEQ_ROWS; ++i) {
         const long long m = m0 + i * high;
         if (m >= M) continue;
-        float v[8];
+        float v[E];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<signed char>((j < 4 ? w[i].x : w[i].y) >> (8 * (j & 3)))) * s[i];
-        store8(y + m * ldy + k, wide_y && n >= 8, n, v);
+        for (int j = 0; j < E; ++j) v[j] = static_cast<float>(static_cast<signed char>(w[i][j / 4] >> (8 * (j & 3)))) * s[i];
+        store16(y + m * ldy + k, wide_y && n >= E, n, v);
     }
 }
 
 template <class Kernel, class... Args>
-cudaError_t launch(Kernel kernel, dim3 grid, int threads, cudaStream_t st, Args... args)
+cudaError_t launch(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t st, Args... args)
 {
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -278,31 +358,64 @@ cudaError_t launch(Kernel kernel, dim3 grid, int threads, cudaStream_t st, Args.
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <class T, bool NORM, bool QUANT, bool WIDE>
-cudaError_t dispatch(const Rows &p, cudaStream_t st)
+constexpr int SM_SMEM = 220 * 1024, SM_THREADS = 1024;      // threads of an SM at 64 registers each
+
+template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
+cudaError_t launch_rows(const Rows &p, int threads, cudaStream_t st)
+{
+    auto kernel = rows_kernel<T, NORM, QUANT, WARP, LAYOUT, CHUNKS>;
+    static QvggtPerDevice cache;
+    int sms = 0;
+    cudaError_t e = qvggt_configure_kernel(kernel, threads, SM_SMEM, 1, cache, &sms);
+    if (e != cudaSuccess) return e;
+    const long long units = WARP ? (p.M - 1) / WARP_ROWS + 1 : p.M;                       // CTAs that one row each would make
+    const int slot = (NORM && p.r ? 2 : 1) * CHUNKS * Chunk<T, LAYOUT>::WARP_GRANULES * 16 * (threads / 32), per_sm = SM_THREADS / threads;
+    // Rows per CTA: enough for the copies to run ahead, few enough for the SMs, which differ in their way to memory, to share the rows out among
+    // themselves (with every CTA's share fixed, rows of the whole grid apart: 43 968 x 4096, norm with residual 263 us against 212).  About the
+    // root of the CTAs that follow one another on an SM's slot; us with 1 / 2 / 4 / 8 / 16: 10 992 x 1024 norm, residual, codes 17.8 / 16.1 /
+    // 17.4; 10 992 x 4096 64 / 55 / 52 / 53 / 63; 43 968 x 4096 250 / 213 / 193 / 189 / 197; fp32 10 992 x 4096 87 / 88 / 91 / 97 / 107.
+    const long long queue = units / ((long long)sms * per_sm);
+    const int most = sizeof(T) == 4 ? 2 : 8;
+    int turns = 1;
+    while (2 * turns <= most && 4LL * turns * turns <= queue) turns *= 2;
+    // Two rows ahead where little is done with a row (43 968 x 4096: quantizer 98 with one, 86 with two; norm and codes 145 and 155).
+    int depth = SM_SMEM / per_sm / slot, wanted = NORM && QUANT ? 1 : 2;
+    if (depth > wanted) depth = wanted;
+    if (depth > turns) depth = turns;
+    if (depth < 1) depth = 1;
+    const int ctas = (int)((units - 1) / turns + 1);
+    return launch(kernel, dim3(ctas), threads, depth * slot, st, p, turns, depth);
+}
+
+template <class T, bool NORM, bool QUANT, int LAYOUT>
+cudaError_t by_length(const Rows &p, cudaStream_t st)
 {
     const int chunks = (p.K + 7) / 8;
-    if (chunks <= 64) {
-        const dim3 grid((p.M - 1) / WARP_ROWS + 1);
-        if (chunks <= 32) return launch(rows_kernel<T, NORM, QUANT, true, WIDE, 1>, grid, WARP_ROWS * 32, st, p);
-        return launch(rows_kernel<T, NORM, QUANT, true, WIDE, 2>, grid, WARP_ROWS * 32, st, p);
-    }
-    if (chunks <= 2 * MAX_THREADS) return launch(rows_kernel<T, NORM, QUANT, false, WIDE, 2>, dim3(p.M), (chunks + 63) / 64 * 32, st, p);
-    return launch(rows_kernel<T, NORM, QUANT, false, WIDE, 0>, dim3(p.M), MAX_THREADS, st, p);
+    if (chunks <= 32) return launch_rows<T, NORM, QUANT, true, LAYOUT, 1>(p, WARP_ROWS * 32, st);
+    if (chunks <= 64) return launch_rows<T, NORM, QUANT, true, LAYOUT, 2>(p, WARP_ROWS * 32, st);
+    if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, false, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
+    return launch(long_rows_kernel<T, NORM, QUANT, LAYOUT>, dim3(p.M), MAX_THREADS, 0, st, p);
+}
+
+template <class T, bool NORM, bool QUANT>
+cudaError_t by_layout(int layout, const Rows &p, cudaStream_t st)
+{
+    if (layout == element::REGULAR) return by_length<T, NORM, QUANT, element::REGULAR>(p, st);
+    return layout == element::ALIGNED ? by_length<T, NORM, QUANT, element::ALIGNED>(p, st) : by_length<T, NORM, QUANT, element::ANY>(p, st);
 }
 
 template <bool NORM, bool QUANT>
-cudaError_t by_type(int type, bool wide, const Rows &p, cudaStream_t st)
+cudaError_t by_type(int type, int layout, const Rows &p, cudaStream_t st)
 {
-    if (type == QVGGT_BF16) return wide ? dispatch<__nv_bfloat16, NORM, QUANT, true>(p, st) : dispatch<__nv_bfloat16, NORM, QUANT, false>(p, st);
-    if (type == QVGGT_FP16) return wide ? dispatch<__half, NORM, QUANT, true>(p, st) : dispatch<__half, NORM, QUANT, false>(p, st);
-    return wide ? dispatch<float, NORM, QUANT, true>(p, st) : dispatch<float, NORM, QUANT, false>(p, st);
+    if (type == QVGGT_BF16) return by_layout<__nv_bfloat16, NORM, QUANT>(layout, p, st);
+    return type == QVGGT_FP16 ? by_layout<__half, NORM, QUANT>(layout, p, st) : by_layout<float, NORM, QUANT>(layout, p, st);
 }
 
 int bytes_of(int type) { return type == QVGGT_FP32 ? 4 : 2; }
@@ -322,20 +435,23 @@ cudaError_t qvggt_launch_rows(int type, const void *X, long long ldx, const void
     p.x = X; p.r = R; p.h = H; p.y = Y; p.q = Xq8; p.scales = scales; p.gamma = gamma;
     p.ldx = ldx; p.ldr = ldr; p.ldh = ldh; p.ldy = ldy; p.ldq = ldq;
     p.eps = eps; p.M = M; p.K = K;
-    const bool wide = rows_aligned(X, ldx, e, 16) && (!R || rows_aligned(R, ldr, e, 16)) && rows_aligned(gamma, 0, 4, 16);
+    p.one_over_k = 1.0f / (float)K;
+    p.floor_factor = (1.0f / 1e-8f) * 127.0f;
     p.wide_h = rows_aligned(H, ldh, e, 16);
     p.wide_y = rows_aligned(Y, ldy, e, 16);
     p.wide_q = rows_aligned(Xq8, ldq, 1, 8);
-    if (!gamma) return by_type<false, true>(type, wide, p, st);
-    return Xq8 ? by_type<true, true>(type, wide, p, st) : by_type<true, false>(type, wide, p, st);
+    const bool aligned = rows_aligned(X, ldx, e, 16) && (!R || rows_aligned(R, ldr, e, 16)) && rows_aligned(gamma, 0, 4, 16);
+    const int layout = !aligned ? element::ANY : K % 8 == 0 && (!H || p.wide_h) && (!Y || p.wide_y) && (!Xq8 || p.wide_q) ? element::REGULAR : element::ALIGNED;
+    if (!gamma) return by_type<false, true>(type, layout, p, st);
+    return Xq8 ? by_type<true, true>(type, layout, p, st) : by_type<true, false>(type, layout, p, st);
 }
 
 cudaError_t qvggt_launch_dequantize(int type, const signed char *Xq8, long long ldq, const float *scales, int M, int K, void *Y, long long ldy, cudaStream_t st)
 {
     const bool wide_q = rows_aligned(Xq8, ldq, 1, 8), wide_y = rows_aligned(Y, ldy, bytes_of(type), 16);
-    const int chunks = (K + 7) / 8, wide = (chunks + 255) / 256, columns = (chunks + wide - 1) / wide, high = 256 / columns * DEQ_ROWS;
+    const int chunks = (K * bytes_of(type) - 1) / 16 + 1, wide = (chunks + 255) / 256, columns = (chunks + wide - 1) / wide, high = 256 / columns * DEQ_ROWS;
     const dim3 grid((M - 1) / high + 1, wide);
-    if (type == QVGGT_BF16) return launch(dequantize_kernel<__nv_bfloat16>, grid, 256, st, Xq8, ldq, scales, static_cast<__nv_bfloat16 *>(Y), ldy, M, K, columns, wide_q, wide_y);
-    if (type == QVGGT_FP16) return launch(dequantize_kernel<__half>, grid, 256, st, Xq8, ldq, scales, static_cast<__half *>(Y), ldy, M, K, columns, wide_q, wide_y);
-    return launch(dequantize_kernel<float>, grid, 256, st, Xq8, ldq, scales, static_cast<float *>(Y), ldy, M, K, columns, wide_q, wide_y);
+    if (type == QVGGT_BF16) return launch(dequantize_kernel<__nv_bfloat16>, grid, 256, 0, st, Xq8, ldq, scales, static_cast<__nv_bfloat16 *>(Y), ldy, M, K, columns, wide_q, wide_y);
+    if (type == QVGGT_FP16) return launch(dequantize_kernel<__half>, grid, 256, 0, st, Xq8, ldq, scales, static_cast<__half *>(Y), ldy, M, K, columns, wide_q, wide_y);
+    return launch(dequantize_kernel<float>, grid, 256, 0, st, Xq8, ldq, scales, static_cast<float *>(Y), ldy, M, K, columns, wide_q, wide_y);
 }
