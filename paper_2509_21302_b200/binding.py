@@ -514,6 +514,7 @@ def quantize_weights_static(W: torch.Tensor, smooth_c: torch.Tensor, sign_v: tor
 
 
 # ---------------------------------------------------------------- the rotation-free 8-bit path
+# Every function takes its outputs as arguments or makes them; what it makes has rows a multiple of 16 bytes apart (see _new_rows()).
 
 def _rows(t: torch.Tensor, M: int, K: int, dtype: torch.dtype) -> int:
     """Checks a matrix of rows (unit stride along a row) and gives its row stride."""
@@ -528,14 +529,16 @@ def _vector(t: torch.Tensor, n: int, dtype: torch.dtype = torch.float32) -> int:
     return t.data_ptr()
 
 
-def _new_codes(M: int, K: int, device) -> torch.Tensor:
-    """Codes as linear_c8 reads them: rows a multiple of 16 bytes apart."""
-    return torch.empty((M, (K + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :K]
+def _new_rows(M: int, K: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """Rows a multiple of 16 bytes apart (a view, where K elements are no such multiple): as linear_c8 reads codes, and as they are written
+    fastest."""
+    step = 16 // dtype.itemsize
+    return torch.empty((M, (K + step - 1) // step * step), dtype=dtype, device=device)[:, :K]
 
 
 def quantize_c8(X: torch.Tensor, Xq8: torch.Tensor | None = None, a_scale: torch.Tensor | None = None):
     """Rows to 8-bit codes, one scale per row, no rotation: X [M,K] bf16 / fp16 / fp32, any K and row stride -> (Xq8 [M,K] int8, a_scale
-    fp32 [M]).  New codes have rows a multiple of 16 bytes apart (a view, where K is no such multiple), as linear_c8 wants them."""
+    fp32 [M])."""
     if _fast is not None:
         r = _fast.quantize_c8(X, Xq8, a_scale)
         if r is not None:
@@ -544,7 +547,7 @@ def quantize_c8(X: torch.Tensor, Xq8: torch.Tensor | None = None, a_scale: torch
     M, K = X.shape
     ldx = _rows(X, M, K, X.dtype)
     if Xq8 is None:
-        Xq8 = _new_codes(M, K, X.device)
+        Xq8 = _new_rows(M, K, torch.int8, X.device)
     if a_scale is None:
         a_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
     _check(lib().qvggt_quantize_c8(_ptr(X), TYPES[X.dtype], ldx, M, K, _ptr(Xq8), _rows(Xq8, M, K, torch.int8), _vector(a_scale, M), _stream()),
@@ -563,7 +566,7 @@ def dequantize_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, dtype: torch.dtype =
     ldq = _rows(Xq8, M, K, torch.int8)
     if Y is None:
         assert dtype in TYPES
-        Y = torch.empty((M, K), dtype=dtype, device=Xq8.device)
+        Y = _new_rows(M, K, dtype, Xq8.device)
     assert Y.dtype in TYPES
     _check(lib().qvggt_dequantize_c8(_ptr(Xq8), ldq, _vector(a_scale, M), M, K, _ptr(Y), TYPES[Y.dtype], _rows(Y, M, K, Y.dtype), _stream()),
            "qvggt_dequantize_c8")
@@ -576,7 +579,7 @@ def _norm_arguments(X, gamma, residual, H):
     ldx, g = _rows(X, M, K, X.dtype), _vector(gamma, K)
     ldr = 0 if residual is None else _rows(residual, M, K, X.dtype)
     if H is None and residual is not None:
-        H = torch.empty((M, K), dtype=X.dtype, device=X.device)
+        H = _new_rows(M, K, X.dtype, X.device)
     return M, K, ldx, ldr, g, H, 0 if H is None else _rows(H, M, K, X.dtype)
 
 
@@ -590,7 +593,7 @@ def rmsnorm(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: t
             return r
     M, K, ldx, ldr, g, H, ldh = _norm_arguments(X, gamma, residual, H)
     if Y is None:
-        Y = torch.empty((M, K), dtype=X.dtype, device=X.device)
+        Y = _new_rows(M, K, X.dtype, X.device)
     _check(lib().qvggt_rmsnorm(_ptr(X), _ptr(residual), TYPES[X.dtype], ldx, ldr, M, K, g, eps, _ptr(H), ldh, _ptr(Y), _rows(Y, M, K, X.dtype),
                                _stream()), "qvggt_rmsnorm")
     return Y if H is None else (Y, H)
@@ -606,7 +609,7 @@ def rmsnorm_quantize_c8(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6,
             return r
     M, K, ldx, ldr, g, H, ldh = _norm_arguments(X, gamma, residual, H)
     if Xq8 is None:
-        Xq8 = _new_codes(M, K, X.device)
+        Xq8 = _new_rows(M, K, torch.int8, X.device)
     if a_scale is None:
         a_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
     _check(lib().qvggt_rmsnorm_quantize_c8(_ptr(X), _ptr(residual), TYPES[X.dtype], ldx, ldr, M, K, g, eps, _ptr(H), ldh, _ptr(Xq8),
@@ -617,8 +620,7 @@ def rmsnorm_quantize_c8(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6,
 def linear_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, Wq8: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor | None = None,
               dtype: torch.dtype = torch.bfloat16, Y: torch.Tensor | None = None) -> torch.Tensor:
     """Product of 8-bit codes with scales for each token and channel: Xq8 [M,K], Wq8 [N,K] int8 (rows a multiple of 16 bytes apart),
-    a_scale fp32 [M], w_scale fp32 [N], bias [N] of the results' type or None -> Y [M,N] of `dtype` (or of Y's own, where Y is given).
-    A new Y has rows a multiple of 16 bytes apart (a view, where N is no such multiple)."""
+    a_scale fp32 [M], w_scale fp32 [N], bias [N] of the results' type or None -> Y [M,N] of `dtype` (or of Y's own, where Y is given)."""
     if _fast is not None and dtype in TYPES:
         r = _fast.linear_c8(Xq8, a_scale, Wq8, w_scale, bias, TYPES[dtype], Y)
         if r is not None:
@@ -628,8 +630,7 @@ def linear_c8(Xq8: torch.Tensor, a_scale: torch.Tensor, Wq8: torch.Tensor, w_sca
     ldx, ldw = _rows(Xq8, M, K, torch.int8), _rows(Wq8, N, K, torch.int8)
     if Y is None:
         assert dtype in TYPES
-        step = 16 // dtype.itemsize
-        Y = torch.empty((M, (N + step - 1) // step * step), dtype=dtype, device=Xq8.device)[:, :N]
+        Y = _new_rows(M, N, dtype, Xq8.device)
     assert Y.dtype in TYPES
     _check(lib().qvggt_linear_c8(_ptr(Xq8), ldx, _vector(a_scale, M), _ptr(Wq8), ldw, _vector(w_scale, N),
                                  None if bias is None else _vector(bias, N, Y.dtype), M, N, K, _ptr(Y), TYPES[Y.dtype], _rows(Y, M, N, Y.dtype),

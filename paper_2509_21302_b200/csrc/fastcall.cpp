@@ -399,11 +399,11 @@ struct Plain {
     }
     static int64_t ld(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : up(t.size(1), 16); }
     // `given`, or a new matrix whose rows are a multiple of 16 bytes apart.
-    static Tensor or_new(const Tensor &given, int64_t M, int64_t K, const at::TensorOptions &options, int64_t step)
+    static Tensor or_new(const Tensor &given, int64_t M, int64_t K, const at::TensorOptions &options, ScalarType type)
     {
         if (given.defined()) return given;
-        const int64_t width = up(K, step);
-        const Tensor t = at::empty({M, width}, options);
+        const int64_t width = up(K, 16 / static_cast<int64_t>(c10::elementSize(type)));
+        const Tensor t = at::empty({M, width}, options.dtype(type));
         return width == K ? t : t.as_strided({M, K}, {width, 1});
     }
     bool sizes(int64_t M, int64_t K) { return in.ok && M <= INT32_MAX && K >= 1 && K <= INT32_MAX; }
@@ -419,7 +419,7 @@ PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     const int64_t M = X.size(0), K = X.size(1);
     const Tensor &xq = p.matrix(at::kChar, M, K, true), &as = p.vector(at::kFloat, M, true);
     if (!p.in.done()) Py_RETURN_NONE;
-    const Tensor q = Plain::or_new(xq, M, K, X.options().dtype(at::kChar), 16), a = as.defined() ? as : at::empty({M}, X.options().dtype(at::kFloat));
+    const Tensor q = Plain::or_new(xq, M, K, X.options(), at::kChar), a = as.defined() ? as : at::empty({M}, X.options().dtype(at::kFloat));
     const void *x = X.data_ptr();
     S8 *qp = static_cast<S8 *>(q.data_ptr());
     float *ap = static_cast<float *>(a.data_ptr());
@@ -443,7 +443,7 @@ PyObject *dequantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     const int64_t wanted = p.in.integer();
     const Tensor &given = p.matrix(true);
     if (!p.in.done() || (given.defined() && (given.size(0) != M || given.size(1) != K))) Py_RETURN_NONE;
-    const Tensor y = given.defined() ? given : at::empty({M, K}, xq.options().dtype(scalar_type(wanted)));
+    const Tensor y = Plain::or_new(given, M, K, xq.options(), scalar_type(wanted));
     const int type = type_code(y.scalar_type());
     if (type < 0) Py_RETURN_NONE;
     const S8 *qp = static_cast<const S8 *>(xq.data_ptr());
@@ -472,8 +472,8 @@ PyObject *rmsnorm_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     const Tensor &as = QUANT ? p.vector(at::kFloat, M, true) : none, &hg = p.matrix(T, M, K, true);
     if (!p.in.done()) Py_RETURN_NONE;
     const bool sum = R.defined() || hg.defined();
-    const Tensor h = hg.defined() || !sum ? hg : at::empty({M, K}, X.options());
-    const Tensor y = QUANT ? Plain::or_new(out, M, K, X.options().dtype(at::kChar), 16) : out.defined() ? out : at::empty({M, K}, X.options());
+    const Tensor h = sum ? Plain::or_new(hg, M, K, X.options(), T) : hg;
+    const Tensor y = Plain::or_new(out, M, K, X.options(), QUANT ? at::kChar : T);
     const Tensor a = !QUANT || as.defined() ? as : at::empty({M}, X.options().dtype(at::kFloat));
     const void *x = X.data_ptr(), *r = R.defined() ? R.data_ptr() : nullptr;
     const float *gp = static_cast<const float *>(gamma.data_ptr());
@@ -514,7 +514,7 @@ PyObject *linear_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     const int type = type_code(T);
     if (type < 0 || (bias.defined() && !(bias.scalar_type() == T && bias.dim() == 1 && bias.size(0) == N && bias.is_contiguous() && bias.get_device() == p.st.device_index())))
         Py_RETURN_NONE;
-    const Tensor y = Plain::or_new(given, M, N, xq.options().dtype(T), type == QVGGT_FP32 ? 4 : 8);
+    const Tensor y = Plain::or_new(given, M, N, xq.options(), T);
     const S8 *qp = static_cast<const S8 *>(xq.data_ptr()), *wp = static_cast<const S8 *>(wq.data_ptr());
     const float *ap = static_cast<const float *>(as.data_ptr()), *sp = static_cast<const float *>(ws.data_ptr());
     const void *bp = bias.defined() ? bias.data_ptr() : nullptr;

@@ -155,7 +155,7 @@ __device__ __forceinline__ void async_wait(int pending)       // at most so many
 
 // Rows in registers: thread t of a row's threads (a warp, or the CTA) has the chunks t, t + threads, .. (CHUNKS of them).  A warp or CTA
 // takes `turns` rows; while one is worked on, the next `depth` are on their way to shared memory, each warp fetching what it will read
-// itself, so that no warp waits for another but in the reduction.  gamma stays in registers.
+// itself, so that no warp waits for another but in the reduction.  gamma comes from L1 for every row.
 template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
 __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (CHUNKS > 1 ? 3 : 4) : 1) rows_kernel(const __grid_constant__ Rows p, int turns, int depth)
 {
@@ -198,14 +198,12 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
         async_commit();
     };
     for (int d = 0; d < depth; ++d) fetch(d, mine + d * slot_bytes);
-    uint64_t g[CHUNKS][4] = {};
+    if (LAYOUT == REGULAR)                                                   // what no copy writes is read as zero
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i)
-        if (NORM && n[i] > 0) {
-            Chunk<float, LAYOUT> c;
-            c.fetch(p.gamma + at[i], n[i]);
-            c.get(p.gamma + at[i], n[i], g[i]);
-        }
+        for (int i = 0; i < CHUNKS; ++i)
+            for (uint32_t a = mine + i * BLOCK; n[i] <= 0 && a < mine + depth * slot_bytes; a += TENSOR)
+#pragma unroll
+                for (int j = 0; j < C::SPAN; ++j) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(a + (lane * C::SPAN + j) * 16), "r"(0) : "memory");
     uint32_t slot = mine;
     for (int turn = 0; turn < rows; ++turn) {
         Row<T, NORM, QUANT, LAYOUT> row;
@@ -224,17 +222,24 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[i][j] = ptx::f32x2_add(v[i][j], a[j]);
             }
-            if (LAYOUT == REGULAR && n[i] <= 0)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[i][j] = 0;
         }
         __syncwarp();                                                        // every lane has read the slot that is fetched into now
         fetch(turn + depth, slot);
         slot = slot == mine && depth > 1 ? mine + slot_bytes : mine;
+        // (of a chunk beyond the row, whose values are zeros, the row's first gammas: no choice between loads, and nothing that the row
+        // does not meet anyway)
+        auto gamma = [&](int i, uint64_t (&g)[4]) {
+            const int a = n[i] > 0 ? at[i] : 0;
+            Chunk<float, LAYOUT> c;
+            c.fetch(p.gamma + a, p.K - a);
+            c.get(p.gamma + a, p.K - a, g);
+        };
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i) {
             if (NORM && p.h && n[i] > 0) store8(h + at[i], LAYOUT == REGULAR || (p.wide_h && n[i] >= 8), n[i], v[i]);
-            row.take(v[i], g[i]);
+            uint64_t g[4];
+            if (NORM && QUANT) gamma(i, g);
+            row.take(v[i], g);
         }
         reduce_row<WARP, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
         row.end(p, scale);
@@ -242,7 +247,11 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
         for (int i = 0; i < CHUNKS; ++i)
             if (n[i] > 0) {
                 if constexpr (QUANT) row.store(q + at[i], p.wide_q, n[i], v[i], one2);
-                else row.store(y + at[i], p.wide_y, n[i], v[i], g[i]);
+                else {
+                    uint64_t g[4];
+                    gamma(i, g);
+                    row.store(y + at[i], p.wide_y, n[i], v[i], g);
+                }
             }
         if (LAYOUT == ANY) { x += step * p.ldx; r += step * p.ldr; }         // (only where the row begins in its granule is asked of them)
         if (NORM) h += step * p.ldh;
@@ -367,6 +376,10 @@ cudaError_t launch(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t
 
 constexpr int SM_SMEM = 220 * 1024, SM_THREADS = 1024;      // threads of an SM at 64 registers each
 
+// Shared memory of one row ahead, for each warp.
+template <class T, int LAYOUT>
+int ring_bytes(const Rows &p, int chunks) { return (p.r ? 2 : 1) * chunks * Chunk<T, LAYOUT>::WARP_GRANULES * 16; }
+
 template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
 cudaError_t launch_rows(const Rows &p, int threads, cudaStream_t st)
 {
@@ -376,7 +389,7 @@ cudaError_t launch_rows(const Rows &p, int threads, cudaStream_t st)
     cudaError_t e = qvggt_configure_kernel(kernel, threads, SM_SMEM, 1, cache, &sms);
     if (e != cudaSuccess) return e;
     const long long units = WARP ? (p.M - 1) / WARP_ROWS + 1 : p.M;                       // CTAs that one row each would make
-    const int slot = (NORM && p.r ? 2 : 1) * CHUNKS * Chunk<T, LAYOUT>::WARP_GRANULES * 16 * (threads / 32), per_sm = SM_THREADS / threads;
+    const int slot = threads / 32 * ring_bytes<T, LAYOUT>(p, CHUNKS), per_sm = SM_THREADS / threads;
     // Rows per CTA: enough for the copies to run ahead, few enough for the SMs, which differ in their way to memory, to share the rows out among
     // themselves (with every CTA's share fixed, rows of the whole grid apart: 43 968 x 4096, norm with residual 263 us against 212).  About the
     // root of the CTAs that follow one another on an SM's slot; us with 1 / 2 / 4 / 8 / 16: 10 992 x 1024 norm, residual, codes 17.8 / 16.1 /
@@ -400,6 +413,10 @@ cudaError_t by_length(const Rows &p, cudaStream_t st)
     const int chunks = (p.K + 7) / 8;
     if (chunks <= 32) return launch_rows<T, NORM, QUANT, true, LAYOUT, 1>(p, WARP_ROWS * 32, st);
     if (chunks <= 64) return launch_rows<T, NORM, QUANT, true, LAYOUT, 2>(p, WARP_ROWS * 32, st);
+    // Four chunks a thread, half the warps, where arithmetic shows beside the little that is read: every warp spends some 250 instructions
+    // a row on what does not depend on its chunks.  43 968 x 4096 bf16, us with two / four: norm and codes 121 / 110, quantizer 80 / 80;
+    // 10 992 x 4096 33 / 30 and 22.7 / 20.9; but with a residual 50 / 52, norm alone 32 / 32, one row 1.9 / 2.5.
+    if (QUANT && !p.r && p.M >= 4096 && chunks > 128 && chunks <= 4 * MAX_THREADS) return launch_rows<T, NORM, QUANT, false, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
     if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, false, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
     return launch(long_rows_kernel<T, NORM, QUANT, LAYOUT>, dim3(p.M), MAX_THREADS, 0, st, p);
 }
