@@ -37,11 +37,11 @@ __device__ __forceinline__ uint4 ld_cluster(uint32_t addr)
     return v;
 }
 
-// One tile of CH channels x tok tokens per cluster of `split` CTAs; blockIdx.x = tile * split + rank, blockIdx.y = tile of tokens.
-template <class T>
+// One tile of CH channels x tok tokens per cluster of SPLIT CTAs; blockIdx.x = tile * SPLIT + rank, blockIdx.y = tile of tokens.
+template <class T, int SPLIT>
 __global__ void __launch_bounds__(WARPS * 32)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const float *__restrict__ a_scale, const float *__restrict__ w_scale,
-                    const T *__restrict__ bias, T *__restrict__ Y, long long ldy, int M, int N, int K, int tok, int stages, int split, int tmem_cols)
+                    const T *__restrict__ bias, T *__restrict__ Y, long long ldy, int M, int N, int K, int tok, int stages, int tmem_cols)
 {
     int *status = &split_status;
     extern __shared__ unsigned char smem_raw[];
@@ -51,10 +51,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + OFF_TMEM);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + OFF_ABORT);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = split > 1 ? (int)ptx::cluster_ctarank() : 0;
-    const int n0 = (int)(blockIdx.x / split) * CH;
+    const int rank = SPLIT > 1 ? (int)ptx::cluster_ctarank() : 0;
+    const int n0 = (int)(blockIdx.x / SPLIT) * CH;
     const int m0 = blockIdx.y * tok, rows = min(tok, M - m0);
-    const int KB = (K + BK - 1) / BK, first = (int)((long long)KB * rank / split), blocks = (int)((long long)KB * (rank + 1) / split) - first;
+    const int KB = (K + BK - 1) / BK, first = KB * rank / SPLIT, blocks = KB * (rank + 1) / SPLIT - first;
     const int stage_bytes = W_BYTES + tok * BK;
 
     if (threadIdx.x == 0) {
@@ -70,8 +70,13 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *s_tmem;
-    ptx::grid_dependency_wait();
+    // The next kernel of the stream may set itself up, and the weights may be on their way to L2, while the previous one ends: a prefetch
+    // neither sees nor changes what that may still write.
     ptx::grid_launch_dependents();
+    if (warp == 0 && ptx::elect_one())
+        for (int i = 0; i < blocks; ++i) ptx::tma_prefetch_2d(&map_w, (first + i) * BK, n0);
+    __syncwarp();
+    ptx::grid_dependency_wait();
 
     if (warp == 0) {
         if (ptx::elect_one()) {
@@ -114,16 +119,22 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     ptx::tc_fence_after_sync();
     if (alive) {
         const int quarter = warp & 3;
-        for (int c = (warp >> 2) * 16; c < rows; c += 32) {
-            uint32_t raw[16];
-            ptx::tmem_ld_32x16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, raw);
+        for (int c = (warp >> 2) * 16; c < rows; c += 64) {
+            uint32_t raw[2][16];
+            const uint32_t at = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c;
+            const bool more = c + 32 < rows;
+            ptx::tmem_ld_32x16(at, raw[0]);
+            if (more) ptx::tmem_ld_32x16(at + 32, raw[1]);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) part[(c + j) * CH + quarter * 32 + lane] = static_cast<int>(raw[j]);
+            for (int j = 0; j < 16; ++j) part[(c + j) * CH + quarter * 32 + lane] = static_cast<int>(raw[0][j]);
+            if (more)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) part[(c + 32 + j) * CH + quarter * 32 + lane] = static_cast<int>(raw[1][j]);
         }
     }
     ptx::tc_fence_before_sync();
-    if (split > 1) ptx::cluster_sync();
+    if (SPLIT > 1) ptx::cluster_sync();
     else __syncthreads();
 
     // A warp finishes a token at a time, four channels a lane; the cluster's CTAs take turns.
@@ -135,30 +146,41 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             ws[i] = n + i < N ? __ldg(w_scale + n + i) : 0.0f;
             bs[i] = bias && n + i < N ? element::to_float(bias[n + i]) : 0.0f;
         }
-        for (int r = warp * split + rank; r < rows; r += WARPS * split) {
-            const uint32_t at = ops + (r * CH + c) * 4;
-            int s[4] = {0, 0, 0, 0};
-            for (int k = 0; k < split; ++k) {
-                const uint4 v = ld_cluster(ptx::map_to_cta(at, k));
-                s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+        constexpr int AT_ONCE = SPLIT == 8 ? 2 : 4, STEP = WARPS * SPLIT;          // tokens whose sums are on their way together
+        for (int r0 = warp * SPLIT + rank; r0 < rows; r0 += AT_ONCE * STEP) {
+            uint4 v[AT_ONCE][SPLIT];
+            float as[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int r = r0 + j * STEP;
+                if (r >= rows) break;
+                as[j] = __ldg(a_scale + m0 + r);
+#pragma unroll
+                for (int k = 0; k < SPLIT; ++k) v[j][k] = ld_cluster(ptx::map_to_cta(ops + (r * CH + c) * 4, k));
             }
-            const long long m = m0 + r;
-            const float as = __ldg(a_scale + m);
-            float z[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] = __fmaf_rn(static_cast<float>(s[i]), __fmul_rn(as, ws[i]), bs[i]);
-            T *y = Y + m * ldy + n;
-            if (n + 4 <= N && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(T) - 1)) == 0) {
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(y) = make_float4(z[0], z[1], z[2], z[3]);
-                else *reinterpret_cast<uint2 *>(y) = make_uint2(element::pack2<T>(z[0], z[1]), element::pack2<T>(z[2], z[3]));
-            } else {
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int r = r0 + j * STEP;
+                if (r >= rows) break;
+                int s[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n + i < N) y[i] = element::from_float<T>(z[i]);
+                for (int k = 0; k < SPLIT; ++k) { s[0] += v[j][k].x; s[1] += v[j][k].y; s[2] += v[j][k].z; s[3] += v[j][k].w; }
+                float z[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = __fmaf_rn(static_cast<float>(s[i]), __fmul_rn(as[j], ws[i]), bs[i]);
+                T *y = Y + (long long)(m0 + r) * ldy + n;
+                if (n + 4 <= N && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(T) - 1)) == 0) {
+                    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(y) = make_float4(z[0], z[1], z[2], z[3]);
+                    else *reinterpret_cast<uint2 *>(y) = make_uint2(element::pack2<T>(z[0], z[1]), element::pack2<T>(z[2], z[3]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (n + i < N) y[i] = element::from_float<T>(z[i]);
+                }
             }
         }
     }
-    if (split > 1) ptx::cluster_sync_relaxed();        // a CTA's sums stay until its peers have read them
+    if (SPLIT > 1) ptx::cluster_sync_relaxed();        // a CTA's sums stay until its peers have read them
     else __syncthreads();
     if (warp == 1) {
         ptx::tc_fence_after_sync();
@@ -171,24 +193,22 @@ int round_up(int n, int step) { return (n + step - 1) / step * step; }
 constexpr int SMEM_FULL = 232448 - 2048;      // stages of a CTA that has its SM to itself, and of one that shares it
 constexpr int SMEM_HALF = 232448 / 2 - 4096;
 
-template <class T>
-cudaError_t launch(const QvggtLinear &p, int split, cudaStream_t st)
+template <class T, int SPLIT>
+cudaError_t launch(const QvggtLinear &p, cudaStream_t st)
 {
     static QvggtPerDevice cache;
     int sms = 0;
-    cudaError_t e = qvggt_configure_kernel(linear_split_kernel<T>, WARPS * 32, OFF_OPS + SMEM_FULL + 1024, 1, cache, &sms);
+    cudaError_t e = qvggt_configure_kernel(linear_split_kernel<T, SPLIT>, WARPS * 32, OFF_OPS + SMEM_FULL + 1024, 1, cache, &sms);
     if (e != cudaSuccess) return e;
-    if (p.M > 65535 * MAX_TOK) return cudaErrorNotSupported;
     const int row_tiles = (p.M - 1) / MAX_TOK + 1, tok = round_up((p.M - 1) / row_tiles + 1, 16), tiles = (p.N - 1) / CH + 1;
     const int KB = (p.K - 1) / BK + 1;
-    if (split == 0)
-        for (split = MAX_SPLIT; split > 1 && ((long long)tiles * row_tiles * split > 2 * sms || KB < 2 * split); split /= 2) {}
-    if (KB < split) return cudaErrorInvalidValue;
+    if (KB < SPLIT || row_tiles > 65535) return cudaErrorNotSupported;
     const int stage_bytes = W_BYTES + tok * BK;
-    const int limit = (long long)tiles * row_tiles * split > sms && 3 * stage_bytes <= SMEM_HALF ? SMEM_HALF : SMEM_FULL;
+    const int blocks = (KB + SPLIT - 1) / SPLIT;
+    const int limit = 3 * stage_bytes <= SMEM_HALF && ((long long)tiles * row_tiles * SPLIT > sms || blocks <= 12) ? SMEM_HALF : SMEM_FULL;
     int stages = limit / stage_bytes;
     if (stages > MAX_STAGES) stages = MAX_STAGES;
-    if (stages > (KB + split - 1) / split) stages = (KB + split - 1) / split;
+    if (stages > blocks) stages = blocks;
     int ops = stages * stage_bytes;
     if (ops < tok * CH * 4) ops = tok * CH * 4;
     int tmem_cols = 32;
@@ -199,26 +219,41 @@ cudaError_t launch(const QvggtLinear &p, int split, cudaStream_t st)
         return cudaErrorInvalidValue;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = SPLIT; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * split, row_tiles);
+    cfg.gridDim = dim3(tiles * SPLIT, row_tiles);
     cfg.blockDim = dim3(WARPS * 32);
     cfg.dynamicSmemBytes = OFF_OPS + ops + 1024;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, linear_split_kernel<T>, map_w, map_x, p.a_scale, p.w_scale, static_cast<const T *>(p.bias), static_cast<T *>(p.Y), p.ldy,
-                              p.M, p.N, p.K, tok, stages, split, tmem_cols);
+    return cudaLaunchKernelEx(&cfg, linear_split_kernel<T, SPLIT>, map_w, map_x, p.a_scale, p.w_scale, static_cast<const T *>(p.bias), static_cast<T *>(p.Y), p.ldy,
+                              p.M, p.N, p.K, tok, stages, tmem_cols);
+}
+
+template <class T>
+cudaError_t by_split(const QvggtLinear &p, int split, cudaStream_t st)
+{
+    return split == 8 ? launch<T, 8>(p, st) : split == 4 ? launch<T, 4>(p, st) : split == 2 ? launch<T, 2>(p, st) : launch<T, 1>(p, st);
 }
 
 }  // namespace
 
 cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, int split, cudaStream_t st)
 {
-    if (p.type == QVGGT_BF16) return launch<__nv_bfloat16>(p, split, st);
-    return p.type == QVGGT_FP16 ? launch<__half>(p, split, st) : launch<float>(p, split, st);
+    if (split == 0) {
+        // As many CTAs as ask for the weights faster than fewer would, but the partial sums are paid for by the token (distributed shared
+        // memory): us at 1 / 32 / 64 / 128 rows with 2, 4, 8 CTAs a tile: N = K = 4096 (32 tiles) 6.0 6.5 7.0 8.3, 5.4 6.0 7.3 10.2, 5.5 6.6 8.0
+        // 11.1; N = 1024, K = 4096 (8 tiles) 5.0 5.4 5.9 7.2, 3.9 4.3 5.1 6.8, 3.4 4.0 4.7 6.9; N = 2048, K = 8192 (16) 8.5 9.0 9.6 11.8, 6.0 6.4 7.0
+        // 8.5, 5.5 6.3 7.6 10.6; N = 5003, K = 2011 (40) 5.2 5.7 6.6 8.4, 4.3 5.1 6.6 9.7, 7.1 8.5 10.4 14.8; N = 16 384 (128) 1: 13.7, 2: 13.7, 4: 15.4.
+        const int KB = (p.K - 1) / BK + 1, sms = qvggt_sm_count();
+        const long long tiles = ((p.N - 1) / CH + 1) * (long long)((p.M - 1) / MAX_TOK + 1), most = p.M <= 32 ? sms + sms / 4 : p.M <= 64 ? sms : sms / 2;
+        for (split = MAX_SPLIT; split > 1 && (tiles * split > most || KB < 2 * split); split /= 2) {}
+    }
+    if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, split, st);
+    return p.type == QVGGT_FP16 ? by_split<__half>(p, split, st) : by_split<float>(p, split, st);
 }
 
 cudaError_t qvggt_read_split_status(int *code) { return cudaMemcpyFromSymbol(code, split_status, sizeof(int)); }
