@@ -205,7 +205,9 @@ cudaError_t launch(const QvggtLinear &p, cudaStream_t st)
     if (KB < SPLIT || row_tiles > 65535) return cudaErrorNotSupported;
     const int stage_bytes = W_BYTES + tok * BK;
     const int blocks = (KB + SPLIT - 1) / SPLIT;
-    const int limit = 3 * stage_bytes <= SMEM_HALF && ((long long)tiles * row_tiles * SPLIT > sms || blocks <= 12) ? SMEM_HALF : SMEM_FULL;
+    // Half of the SM, so that the next kernel's CTAs, or this one's, set themselves up beside it -- where five stages fit (three: N = K = 4096, 128
+    // rows 10.2 us instead of 8.1), and no long stream would do with fewer than the whole SM holds (N = 16 384, K = 4096 18.8 instead of 13.4).
+    const int limit = (blocks < 5 ? blocks : 5) * stage_bytes <= SMEM_HALF && ((long long)tiles * row_tiles * SPLIT > sms || blocks <= 12) ? SMEM_HALF : SMEM_FULL;
     int stages = limit / stage_bytes;
     if (stages > MAX_STAGES) stages = MAX_STAGES;
     if (stages > blocks) stages = blocks;
@@ -244,13 +246,13 @@ cudaError_t by_split(const QvggtLinear &p, int split, cudaStream_t st)
 cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, int split, cudaStream_t st)
 {
     if (split == 0) {
-        // As many CTAs as ask for the weights faster than fewer would, but the partial sums are paid for by the token (distributed shared
-        // memory): us at 1 / 32 / 64 / 128 rows with 2, 4, 8 CTAs a tile: N = K = 4096 (32 tiles) 6.0 6.5 7.0 8.3, 5.4 6.0 7.3 10.2, 5.5 6.6 8.0
-        // 11.1; N = 1024, K = 4096 (8 tiles) 5.0 5.4 5.9 7.2, 3.9 4.3 5.1 6.8, 3.4 4.0 4.7 6.9; N = 2048, K = 8192 (16) 8.5 9.0 9.6 11.8, 6.0 6.4 7.0
-        // 8.5, 5.5 6.3 7.6 10.6; N = 5003, K = 2011 (40) 5.2 5.7 6.6 8.4, 4.3 5.1 6.6 9.7, 7.1 8.5 10.4 14.8; N = 16 384 (128) 1: 13.7, 2: 13.7, 4: 15.4.
+        // As many CTAs as ask for the weights faster than fewer would; clusters of eight that have their SMs to themselves find room for a few only.
+        // us at 1 / 32 / 64 / 128 rows with 2, 4, 8 CTAs a tile: N = K = 4096 (32 tiles) 6.0 6.4 6.9 8.2, 5.4 6.0 6.7 8.1, 5.4 6.4 7.9 19;
+        // N = 1024, K = 4096 (8 tiles) 5.0 5.4 5.9 7.2, 3.9 4.3 4.8 6.2, 3.4 4.0 4.7 6.0; N = 2048, K = 8192 (16) 8.6 9.0 9.7 11.7, 5.8 6.3 6.9 8.3, 5.5
+        // 6.2 11.3 14.2; N = 5003, K = 2011 (40) 5.2 5.8 5.8 7.5, 4.3 5.1 6.6 12.7, 7.2 8.5 10.4 14.6; N = 16 384 (128) one 13.7, two 13.7, four 15.4.
         const int KB = (p.K - 1) / BK + 1, sms = qvggt_sm_count();
-        const long long tiles = ((p.N - 1) / CH + 1) * (long long)((p.M - 1) / MAX_TOK + 1), most = p.M <= 32 ? sms + sms / 4 : p.M <= 64 ? sms : sms / 2;
-        for (split = MAX_SPLIT; split > 1 && (tiles * split > most || KB < 2 * split); split /= 2) {}
+        const long long tiles = ((p.N - 1) / CH + 1) * (long long)((p.M - 1) / MAX_TOK + 1);
+        for (split = tiles <= sms / 16 ? MAX_SPLIT : 4; split > 1 && (tiles * split > (p.M <= 32 ? sms + sms / 4 : sms) || KB < 2 * split); split /= 2) {}
     }
     if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, split, st);
     return p.type == QVGGT_FP16 ? by_split<__half>(p, split, st) : by_split<float>(p, split, st);
