@@ -66,24 +66,25 @@ struct Chunk {
             w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
         }
     }
-    // The granules of 32 chunks in a row, for the 32 lanes of a warp: asynchronous copies of neighbouring granules by neighbouring lanes
-    // (a granule of its own chunk's each would fetch every 32-byte sector of fp32, and of misaligned rows, twice).  p: lane 0's first
-    // element, n: elements of the row from there on, those behind the 32nd chunk included.  Lanes then read their own, behind a wait of
-    // every lane for its copies and a __syncwarp().
-    static constexpr int WARP_GRANULES = 32 * SPAN + (LAYOUT == ANY ? 1 : 0);
+    // The granules of LANES chunks in a row, for so many lanes: asynchronous copies of neighbouring granules by neighbouring lanes (a granule
+    // of its own chunk's each would fetch every 32-byte sector of fp32, and of misaligned rows, twice).  p: lane 0's first element, n:
+    // elements of the row from there on, those behind the last lane's chunk included.  Lanes then read their own, behind a wait of every
+    // lane for its copies and a __syncwarp().
+    template <int LANES> static constexpr int GRANULES = LANES * SPAN + (LAYOUT == ANY ? 1 : 0);
+    template <int LANES>
     __device__ __forceinline__ static void fetch_async(uint32_t smem, const T *p, int n, int lane)
     {
         if constexpr (LAYOUT != ANY) {
             constexpr int E = 16 / sizeof(T);                            // elements of a granule
 #pragma unroll
             for (int i = 0; i < SPAN; ++i)
-                if (n > E * (lane + 32 * i)) async_copy16(smem + (lane + 32 * i) * 16, p + E * (lane + 32 * i));
+                if (n > E * (lane + LANES * i)) async_copy16(smem + (lane + LANES * i) * 16, p + E * (lane + LANES * i));
         } else {
             const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
             const int granules = n > 0 ? static_cast<int>((at & 15) + static_cast<uint32_t>(n) * sizeof(T) + 15) / 16 : 0;
 #pragma unroll
-            for (int i = 0; i < (WARP_GRANULES + 31) / 32; ++i)
-                if (lane + 32 * i < min(granules, WARP_GRANULES)) async_copy16(smem + (lane + 32 * i) * 16, reinterpret_cast<const void *>(base + 16 * (lane + 32 * i)));
+            for (int i = 0; i < (GRANULES<LANES> + LANES - 1) / LANES; ++i)
+                if (lane + LANES * i < min(granules, GRANULES<LANES>)) async_copy16(smem + (lane + LANES * i) * 16, reinterpret_cast<const void *>(base + 16 * (lane + LANES * i)));
         }
     }
     __device__ __forceinline__ static void async_copy16(uint32_t smem, const void *p) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p) : "memory"); }

@@ -16,13 +16,14 @@
 
 namespace {
 
+using element::ALIGNED;
 using element::ANY;
 using element::Chunk;
 using element::REGULAR;
 using element::store8;
 using element::store16;
 
-constexpr int WARP_ROWS = 8;               // rows of a CTA where a warp takes a row
+constexpr int SHORT_THREADS = 256;         // of a CTA where a warp, or a part of one, takes a row
 constexpr int MAX_THREADS = 1024;
 
 struct Rows {
@@ -35,26 +36,33 @@ struct Rows {
     float eps, one_over_k, floor_factor;   // floor_factor: 127 * (1 / 1e-8), every operation rounded
     int M, K;
     uint32_t zero;                         // 0, which the compiler cannot know (ptx::f32x2_one)
-    bool wide_h, wide_y, wide_q;           // every row of it begins on a 16-byte boundary (q: 8 bytes)
+    bool wide_h, wide_y, wide_q, wide_g;   // every row of it begins on a 16-byte boundary (q: 8 bytes)
 };
 
-// Sum of s and largest of a over `lanes` neighbouring lanes (a power of two).
+// Sum of s and largest of a over `lanes` neighbouring lanes (a power of two; all 32 take part).
 template <bool SUM, bool MAX>
 __device__ __forceinline__ void reduce_lanes(float &s, uint32_t &a, int lanes)
 {
 #pragma unroll
     for (int o = 16; o; o >>= 1)
         if (SUM && o < lanes) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (MAX) a = __reduce_max_sync(0xFFFFFFFFu, a);
+    if (!MAX) return;
+    if (lanes == 32) {
+        a = __reduce_max_sync(0xFFFFFFFFu, a);
+    } else {
+#pragma unroll
+        for (int o = 8; o; o >>= 1)
+            if (o < lanes) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+    }
 }
 
-// The same over the row's threads: a warp, or the CTA, which meets once for both (every thread gets the results; `part` holds 32 pairs that
-// no thread still reads from an earlier call: two meetings back is enough).
-template <bool WARP, bool SUM, bool MAX>
+// The same over the row's threads: LANES of a warp, or (0) the CTA, which meets once for both (every thread gets the results; `part` holds 32
+// pairs that no thread still reads from an earlier call: two meetings back is enough).
+template <int LANES, bool SUM, bool MAX>
 __device__ __forceinline__ void reduce_row(float &s, uint32_t &a, uint2 *part)
 {
-    reduce_lanes<SUM, MAX>(s, a, 32);
-    if (WARP) return;
+    reduce_lanes<SUM, MAX>(s, a, LANES ? LANES : 32);
+    if (LANES) return;
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     if (lane == 0) part[threadIdx.x >> 5] = make_uint2(__float_as_uint(s), a);
     __syncthreads();
@@ -62,7 +70,25 @@ __device__ __forceinline__ void reduce_row(float &s, uint32_t &a, uint2 *part)
     const uint2 v = mine < warps ? part[mine] : make_uint2(0, 0);
     s = __uint_as_float(v.x);
     a = v.y;
-    reduce_lanes<SUM, MAX>(s, a, lanes);
+    reduce_lanes<SUM, false>(s, a, lanes);
+    if (MAX) a = __reduce_max_sync(0xFFFFFFFFu, a);
+}
+
+// gamma of a chunk, n (> 0) elements from its first on.  It is aligned as good as always, whatever the rows are.
+template <int LAYOUT>
+__device__ __forceinline__ void load_gamma(const float *gamma, bool wide, int n, uint64_t (&g)[4])
+{
+    if (LAYOUT == REGULAR || wide) {
+        Chunk<float, LAYOUT == ANY ? ALIGNED : LAYOUT> c;
+        c.fetch(gamma, n);
+        c.get(gamma, n, g);
+    } else {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? __ldg(gamma + i) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = ptx::f32x2_pack(f[2 * i], f[2 * i + 1]);
+    }
 }
 
 // The arithmetic on a row's chunks of eight elements, two elements in a word; the same in both kernels below.
@@ -153,24 +179,25 @@ __device__ __forceinline__ void async_wait(int pending)       // at most so many
     else asm volatile("cp.async.wait_group 1;" ::: "memory");
 }
 
-// Rows in registers: thread t of a row's threads (a warp, or the CTA) has the chunks t, t + threads, .. (CHUNKS of them).  A warp or CTA
-// takes `turns` rows; while one is worked on, the next `depth` are on their way to shared memory, each warp fetching what it will read
-// itself, so that no warp waits for another but in the reduction.  gamma comes from L1 for every row.
-template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
-__global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (CHUNKS > 1 ? 3 : 4) : 1) rows_kernel(const __grid_constant__ Rows p, int turns, int depth)
+// Rows in registers: thread t of a row's threads (LANES of a warp, or (0) the CTA) has the chunks t, t + threads, .. (CHUNKS of them).  Its
+// threads take `turns` rows; while one is worked on, the next `depth` are on their way to shared memory, each warp fetching what it will
+// read itself, so that no warp waits for another but in the reduction.  gamma comes from L1 for every row.
+template <class T, bool NORM, bool QUANT, int LANES, int LAYOUT, int CHUNKS>
+__global__ void __launch_bounds__(LANES ? SHORT_THREADS : MAX_THREADS, LANES ? (CHUNKS > 1 ? 3 : 4) : 1) rows_kernel(const __grid_constant__ Rows p, int turns, int depth)
 {
     using C = Chunk<T, LAYOUT>;
-    constexpr uint32_t BLOCK = C::WARP_GRANULES * 16, TENSOR = CHUNKS * BLOCK;
-    extern __shared__ uint4 ring[];                                          // [warp][depth][x, r][CHUNKS][granules]
+    constexpr int GROUP = LANES ? LANES : 32, step = LANES ? SHORT_THREADS / GROUP : 1;      // lanes that fetch together; rows of a CTA at once
+    constexpr uint32_t BLOCK = C::template GRANULES<GROUP> * 16, TENSOR = CHUNKS * BLOCK;
+    extern __shared__ uint4 ring[];                                          // [group][depth][x, r][CHUNKS][granules]
     __shared__ uint2 part[2][32];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    constexpr int step = WARP ? WARP_ROWS : 1;
-    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x, lane = threadIdx.x & 31;
+    const int t = LANES ? threadIdx.x % GROUP : threadIdx.x, threads = LANES ? GROUP : blockDim.x, lane = threadIdx.x % GROUP;
     const bool residual = NORM && p.r;
-    const uint32_t slot_bytes = residual ? 2 * TENSOR : TENSOR, mine = ptx::smem_addr(ring) + (threadIdx.x >> 5) * depth * slot_bytes;
-    const long long m0 = (long long)blockIdx.x * turns * step + (WARP ? threadIdx.x >> 5 : 0), left = (p.M - m0 + step - 1) / step;
-    const int rows = left < turns ? (int)left : turns;                       // of this warp or CTA
+    const uint32_t slot_bytes = residual ? 2 * TENSOR : TENSOR, mine = ptx::smem_addr(ring) + threadIdx.x / GROUP * depth * slot_bytes;
+    const long long first = (long long)blockIdx.x * turns * step, left = (p.M - first + step - 1) / step, m0 = first + (LANES ? threadIdx.x / GROUP : 0);
+    const int rows = left < turns ? (int)left : turns;                       // turns of this CTA
+    const int mine_rows = (int)min((long long)rows, (p.M - m0 + step - 1) / step);       // in the last, a group may have no row
     int at[CHUNKS], n[CHUNKS];                                               // a chunk's first element, elements from there on
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
@@ -185,12 +212,12 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
     const uint64_t one2 = ptx::f32x2_one(p.zero);
 
     auto fetch = [&](int turn, uint32_t slot) {
-        if (turn < rows) {
+        if (turn < mine_rows) {
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
-                const int a = at[i] - 8 * lane;                              // the warp's first
-                C::fetch_async(slot + i * BLOCK, x_ahead + a, p.K - a, lane);
-                if (residual) C::fetch_async(slot + TENSOR + i * BLOCK, r_ahead + a, p.K - a, lane);
+                const int a = at[i] - 8 * lane;                              // the group's first
+                C::template fetch_async<GROUP>(slot + i * BLOCK, x_ahead + a, p.K - a, lane);
+                if (residual) C::template fetch_async<GROUP>(slot + TENSOR + i * BLOCK, r_ahead + a, p.K - a, lane);
             }
             x_ahead += step * p.ldx;
             r_ahead += step * p.ldr;
@@ -207,6 +234,7 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
     uint32_t slot = mine;
     for (int turn = 0; turn < rows; ++turn) {
         Row<T, NORM, QUANT, LAYOUT> row;
+        const bool here = turn < mine_rows;
         uint64_t v[CHUNKS][4];
         async_wait(depth - 1);
         __syncwarp();
@@ -230,22 +258,20 @@ __global__ void __launch_bounds__(WARP ? WARP_ROWS * 32 : MAX_THREADS, WARP ? (C
         // does not meet anyway)
         auto gamma = [&](int i, uint64_t (&g)[4]) {
             const int a = n[i] > 0 ? at[i] : 0;
-            Chunk<float, LAYOUT> c;
-            c.fetch(p.gamma + a, p.K - a);
-            c.get(p.gamma + a, p.K - a, g);
+            load_gamma<LAYOUT>(p.gamma + a, p.wide_g, p.K - a, g);
         };
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i) {
-            if (NORM && p.h && n[i] > 0) store8(h + at[i], LAYOUT == REGULAR || (p.wide_h && n[i] >= 8), n[i], v[i]);
+            if (NORM && p.h && here && n[i] > 0) store8(h + at[i], LAYOUT == REGULAR || (p.wide_h && n[i] >= 8), n[i], v[i]);
             uint64_t g[4];
             if (NORM && QUANT) gamma(i, g);
             row.take(v[i], g);
         }
-        reduce_row<WARP, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
-        row.end(p, scale);
+        reduce_row<LANES, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
+        row.end(p, here ? scale : nullptr);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
-            if (n[i] > 0) {
+            if (here && n[i] > 0) {
                 if constexpr (QUANT) row.store(q + at[i], p.wide_q, n[i], v[i], one2);
                 else {
                     uint64_t g[4];
@@ -275,10 +301,9 @@ __global__ void __launch_bounds__(MAX_THREADS) long_rows_kernel(const __grid_con
     auto load = [&](int at) {
         const int n = p.K - at;
         Chunk<T, LAYOUT> cx, cr;
-        Chunk<float, LAYOUT> cg;
         cx.fetch(x + at, n);
         if (residual) cr.fetch(r + at, n);
-        if (NORM) cg.fetch(p.gamma + at, n);
+        if (NORM) load_gamma<LAYOUT>(p.gamma + at, p.wide_g, n, g);
         cx.get(x + at, n, v);
         if (residual) {
             uint64_t a[4];
@@ -286,10 +311,9 @@ __global__ void __launch_bounds__(MAX_THREADS) long_rows_kernel(const __grid_con
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = ptx::f32x2_add(v[i], a[i]);
         }
-        if (NORM) cg.get(p.gamma + at, n, g);
     };
     for (int at = 8 * threadIdx.x; at < p.K; at += 8 * MAX_THREADS) { load(at); row.take(v, g); }
-    reduce_row<false, NORM, QUANT>(row.sum, row.top, part);
+    reduce_row<0, NORM, QUANT>(row.sum, row.top, part);
     row.end(p, QUANT && threadIdx.x == 0 ? p.scales + m : nullptr);
     const uint64_t one2 = ptx::f32x2_one(p.zero);
     // the sum is stored in the last pass: it may take the place of x or r, which both read
@@ -376,20 +400,21 @@ cudaError_t launch(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t
 
 constexpr int SM_SMEM = 220 * 1024, SM_THREADS = 1024;      // threads of an SM at 64 registers each
 
-// Shared memory of one row ahead, for each warp.
-template <class T, int LAYOUT>
-int ring_bytes(const Rows &p, int chunks) { return (p.r ? 2 : 1) * chunks * Chunk<T, LAYOUT>::WARP_GRANULES * 16; }
+// Shared memory of one row ahead, for each group of lanes that fetches together.
+template <class T, int LAYOUT, int GROUP>
+int ring_bytes(const Rows &p, int chunks) { return (p.r ? 2 : 1) * chunks * Chunk<T, LAYOUT>::template GRANULES<GROUP> * 16; }
 
-template <class T, bool NORM, bool QUANT, bool WARP, int LAYOUT, int CHUNKS>
+template <class T, bool NORM, bool QUANT, int LANES, int LAYOUT, int CHUNKS>
 cudaError_t launch_rows(const Rows &p, int threads, cudaStream_t st)
 {
-    auto kernel = rows_kernel<T, NORM, QUANT, WARP, LAYOUT, CHUNKS>;
+    constexpr int GROUP = LANES ? LANES : 32;
+    auto kernel = rows_kernel<T, NORM, QUANT, LANES, LAYOUT, CHUNKS>;
     static QvggtPerDevice cache;
     int sms = 0;
     cudaError_t e = qvggt_configure_kernel(kernel, threads, SM_SMEM, 1, cache, &sms);
     if (e != cudaSuccess) return e;
-    const long long units = WARP ? (p.M - 1) / WARP_ROWS + 1 : p.M;                       // CTAs that one row each would make
-    const int slot = threads / 32 * ring_bytes<T, LAYOUT>(p, CHUNKS), per_sm = SM_THREADS / threads;
+    const long long units = LANES ? (p.M - 1) / (SHORT_THREADS / GROUP) + 1 : p.M;        // CTAs that one row each would make
+    const int slot = threads / GROUP * ring_bytes<T, LAYOUT, GROUP>(p, CHUNKS), per_sm = SM_THREADS / threads;
     // Rows per CTA: enough for the copies to run ahead, few enough for the SMs, which differ in their way to memory, to share the rows out among
     // themselves (with every CTA's share fixed, rows of the whole grid apart: 43 968 x 4096, norm with residual 263 us against 212).  About the
     // root of the CTAs that follow one another on an SM's slot; us with 1 / 2 / 4 / 8 / 16: 10 992 x 1024 norm, residual, codes 17.8 / 16.1 /
@@ -411,13 +436,15 @@ template <class T, bool NORM, bool QUANT, int LAYOUT>
 cudaError_t by_length(const Rows &p, cudaStream_t st)
 {
     const int chunks = (p.K + 7) / 8;
-    if (chunks <= 32) return launch_rows<T, NORM, QUANT, true, LAYOUT, 1>(p, WARP_ROWS * 32, st);
-    if (chunks <= 64) return launch_rows<T, NORM, QUANT, true, LAYOUT, 2>(p, WARP_ROWS * 32, st);
+    if (chunks <= 8) return launch_rows<T, NORM, QUANT, 8, LAYOUT, 1>(p, SHORT_THREADS, st);
+    if (chunks <= 16) return launch_rows<T, NORM, QUANT, 16, LAYOUT, 1>(p, SHORT_THREADS, st);
+    if (chunks <= 32) return launch_rows<T, NORM, QUANT, 32, LAYOUT, 1>(p, SHORT_THREADS, st);
+    if (chunks <= 64) return launch_rows<T, NORM, QUANT, 32, LAYOUT, 2>(p, SHORT_THREADS, st);
     // Four chunks a thread, half the warps, where arithmetic shows beside the little that is read: every warp spends some 250 instructions
     // a row on what does not depend on its chunks.  43 968 x 4096 bf16, us with two / four: norm and codes 121 / 110, quantizer 80 / 80;
     // 10 992 x 4096 33 / 30 and 22.7 / 20.9; but with a residual 50 / 52, norm alone 32 / 32, one row 1.9 / 2.5.
-    if (QUANT && !p.r && p.M >= 4096 && chunks > 128 && chunks <= 4 * MAX_THREADS) return launch_rows<T, NORM, QUANT, false, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
-    if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, false, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
+    if (QUANT && !p.r && p.M >= 4096 && chunks > 128 && chunks <= 4 * MAX_THREADS) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
+    if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
     return launch(long_rows_kernel<T, NORM, QUANT, LAYOUT>, dim3(p.M), MAX_THREADS, 0, st, p);
 }
 
@@ -457,8 +484,9 @@ cudaError_t qvggt_launch_rows(int type, const void *X, long long ldx, const void
     p.wide_h = rows_aligned(H, ldh, e, 16);
     p.wide_y = rows_aligned(Y, ldy, e, 16);
     p.wide_q = rows_aligned(Xq8, ldq, 1, 8);
-    const bool aligned = rows_aligned(X, ldx, e, 16) && (!R || rows_aligned(R, ldr, e, 16)) && rows_aligned(gamma, 0, 4, 16);
-    const int layout = !aligned ? element::ANY : K % 8 == 0 && (!H || p.wide_h) && (!Y || p.wide_y) && (!Xq8 || p.wide_q) ? element::REGULAR : element::ALIGNED;
+    p.wide_g = rows_aligned(gamma, 0, 4, 16);
+    const bool aligned = rows_aligned(X, ldx, e, 16) && (!R || rows_aligned(R, ldr, e, 16));
+    const int layout = !aligned ? element::ANY : K % 8 == 0 && p.wide_g && (!H || p.wide_h) && (!Y || p.wide_y) && (!Xq8 || p.wide_q) ? element::REGULAR : element::ALIGNED;
     if (!gamma) return by_type<false, true>(type, layout, p, st);
     return Xq8 ? by_type<true, true>(type, layout, p, st) : by_type<true, false>(type, layout, p, st);
 }

@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 TYPES = [torch.bfloat16, torch.float16, torch.float32]
-SIZES = [(1, 1), (3, 7), (1, 8), (9, 9), (2, 64), (17, 255), (8, 257), (33, 512), (5, 1003), (300, 1024), (7, 1025), (4, 2048), (65, 4096), (3, 5001),
+SIZES = [(1, 1), (3, 7), (1, 8), (9, 9), (2, 64), (33, 64), (35, 61), (18, 128), (7, 100), (6001, 64), (5003, 127), (17, 255), (8, 257), (33, 512), (5, 1003), (300, 1024), (7, 1025), (4, 2048), (65, 4096), (3, 5001),
          (2, 16384), (2, 32768), (2, 32776), (1, 131056)]
 
 
@@ -90,7 +90,7 @@ def test_dequantize(M, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("K", [1, 15, 1003, 1024, 3001, 33000])
+@pytest.mark.parametrize("K", [1, 15, 64, 127, 1003, 1024, 3001, 33000])
 @pytest.mark.parametrize("pad,shift", [(5, 0), (0, 1), (8, 8), (3, 3)])
 def test_strides_and_offsets_change_nothing(K, pad, shift, dtype):
     """Any row stride and first element give the results of the aligned layout, and what lies between the rows is left as it was."""
@@ -134,7 +134,7 @@ def test_strides_and_offsets_change_nothing(K, pad, shift, dtype):
     untouched(t2)
 
 
-@pytest.mark.parametrize("K", [100, 1024, 4096, 40000])
+@pytest.mark.parametrize("K", [40, 100, 1024, 4096, 40000])
 def test_in_place(K):
     M, dtype = 6, torch.bfloat16
     gamma = torch.rand(K, device="cuda") + 0.5
