@@ -5,6 +5,7 @@
 // consecutive bytes of a row stand for whichever k the fragment of mma.sync asks for: the same permutation of K for both operands, which
 // an integer sum does not see.  The warps' partial sums meet in shared memory.
 #include "element.cuh"
+#include "linear_plan.cuh"
 #include "qvggt_internal.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
@@ -136,24 +137,14 @@ cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st)
     return p.type == QVGGT_BF16 ? by_rows<__nv_bfloat16>(p, st) : p.type == QVGGT_FP16 ? by_rows<__half>(p, st) : by_rows<float>(p, st);
 }
 
-// Which of the three kernels.  This one starts fastest, but its loads wait for registers: it has the smallest products.  The split kernel streams
-// the weights from all SMs; its time grows with the rows, that of the tiles kernel (gemm_c8.cu) hardly does up to 256 rows, but with K, which
-// one pair of CTAs walks alone.  us, this one / split / tiles (weights from memory):
-//   N = K = 1024          1 row 2.7 / 2.9 / 4.2    16 3.3 / 3.2 / 3.9    32 3.8 / 3.5 / 3.8    64 3.9 / 4.2 / 3.9    128 7.0 / 5.3 / 4.0
-//   N = 1000, K = 520     1 row 2.6 / 3.0 / 3.6    32 3.7 / 3.5 / 3.5    64 3.7 / 4.5 / 3.6
-//   N = 1024, K = 4096    1 row 3.6 / 3.4 / 9.3    64 5.6 / 4.7 / 7.8    128 10.3 / 6.0 / 7.9    256 19.6 / 9.4 / 7.9
-//   N = K = 4096          1 row 10.7 / 5.4 / 14.3  64 23.8 / 6.7 / 9.3   128 39.5 / 8.1 / 9.4    256 72 / 11.4 / 9.5
-//   N = 2048, K = 8192    1 row 10.2 / 5.5 / 16.3  64 22.3 / 6.9 / 14.5  128 39 / 8.3 / 14.6     256 64 / 12.6 / 14.6
-//   N = 8192, K = 1024    1 row 9.0 / 4.1 / 6.7    64 24.6 / 5.6 / 5.6   128 47.7 / 6.0 / 5.2
-//   N = 5003, K = 2011    1 row 7.4 / 4.3 / 10.5   64 20.6 / 5.8 / 8.0   96 - / 6.7 / 6.7        128 36.6 / 7.5 / 6.9
-//   N = 16384, K = 4096   1 row 35 / 13.7 / 20.9   64 84 / 14.9 / 16.2   128 154 / 17.1 / 16.4
-//   512 rows: N = 512, K = 8192 - / 10.8 / 12.9, N = 1024, K = 16 384 - / 17.0 / 24.8, N = K = 4096 138 / 17.6 / 9.5
 cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st)
 {
-    if (p.M <= 8 && (long long)p.N * p.K <= 1 << 21) return qvggt_launch_linear_few(p, st);
-    const bool split = p.M <= 32 || (p.M <= 64 && (p.K > 1024 || p.N > 2048)) || (p.M <= 96 && p.K > 1024) || (p.M <= 128 && p.K >= 3000 && p.N <= 8192) ||
-                       (p.M <= 256 && p.K >= 8192 && p.N <= 2048) || (p.M <= 512 && p.K >= 8192 && p.N <= 1024);
-    cudaError_t e = split ? qvggt_launch_linear_split(p, 0, st) : qvggt_launch_linear_tiles(p, st);
-    if (e == cudaErrorNotSupported) e = qvggt_launch_linear_few(p, st);        // sizes beyond what the others count with
-    return e;
+    const int sms = qvggt_sm_count();
+    if (sms < 1) return cudaErrorInvalidDevice;
+    linear_plan::Split split = {};
+    const linear_plan::Kernel kernel = linear_plan::choose(p.M, p.N, p.K, sms, &split);
+    cudaError_t e = cudaErrorNotSupported;
+    if (kernel == linear_plan::SPLIT) e = qvggt_launch_linear_split(p, split, st);
+    else if (kernel == linear_plan::TILES) e = qvggt_launch_linear_tiles(p, st);
+    return e == cudaErrorNotSupported ? qvggt_launch_linear_few(p, st) : e;       // also for sizes beyond what the others count with
 }

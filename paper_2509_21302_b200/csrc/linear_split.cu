@@ -12,18 +12,19 @@
 
 #include "element.cuh"
 #include "gemm_common.cuh"
+#include "linear_plan.cuh"
 #include "qvggt_internal.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
 
 namespace {
 
-constexpr int CH = 128;                // channels of a tile: rows of the MMA, TMEM lanes
-constexpr int BK = 128;                // codes along K per stage = one 128-byte swizzled row
+using linear_plan::BK;                 // codes along K per stage = one 128-byte swizzled row
+using linear_plan::CH;                 // channels of a tile: rows of the MMA, TMEM lanes
+using linear_plan::MAX_TOK;            // tokens of a tile: columns of the MMA
 constexpr int WARPS = 8;
-constexpr int MAX_TOK = 256;           // tokens of a tile: columns of the MMA, a multiple of 16
 constexpr int MAX_STAGES = 12;
-constexpr int MAX_SPLIT = 8;           // CTAs of a cluster
+static_assert(CH == 128 && BK == 128 && MAX_TOK == 256, "what the instruction descriptor and tensor memory take");
 constexpr int W_BYTES = CH * BK;
 constexpr int OFF_FULL = 0, OFF_EMPTY = OFF_FULL + 8 * MAX_STAGES, OFF_DONE = OFF_EMPTY + 8 * MAX_STAGES, OFF_TMEM = OFF_DONE + 8, OFF_ABORT = OFF_TMEM + 4;
 constexpr int OFF_OPS = 1024;          // stages; then the partial sums [token][channel]
@@ -188,20 +189,17 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     }
 }
 
-int round_up(int n, int step) { return (n + step - 1) / step * step; }
-
 constexpr int SMEM_FULL = 232448 - 2048;      // stages of a CTA that has its SM to itself, and of one that shares it
 constexpr int SMEM_HALF = 232448 / 2 - 4096;
 
 template <class T, int SPLIT>
-cudaError_t launch(const QvggtLinear &p, cudaStream_t st)
+cudaError_t launch(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st)
 {
     static QvggtPerDevice cache;
     int sms = 0;
     cudaError_t e = qvggt_configure_kernel(linear_split_kernel<T, SPLIT>, WARPS * 32, OFF_OPS + SMEM_FULL + 1024, 1, cache, &sms);
     if (e != cudaSuccess) return e;
-    const int row_tiles = (p.M - 1) / MAX_TOK + 1, tok = round_up((p.M - 1) / row_tiles + 1, 16), tiles = (p.N - 1) / CH + 1;
-    const int KB = (p.K - 1) / BK + 1;
+    const int row_tiles = plan.row_tiles, tok = plan.tok, tiles = (int)plan.tiles, KB = (p.K - 1) / BK + 1;
     if (KB < SPLIT || row_tiles > 65535) return cudaErrorNotSupported;
     const int stage_bytes = W_BYTES + tok * BK;
     const int blocks = (KB + SPLIT - 1) / SPLIT;
@@ -236,26 +234,17 @@ cudaError_t launch(const QvggtLinear &p, cudaStream_t st)
 }
 
 template <class T>
-cudaError_t by_split(const QvggtLinear &p, int split, cudaStream_t st)
+cudaError_t by_split(const QvggtLinear &p, const linear_plan::Split &s, cudaStream_t st)
 {
-    return split == 8 ? launch<T, 8>(p, st) : split == 4 ? launch<T, 4>(p, st) : split == 2 ? launch<T, 2>(p, st) : launch<T, 1>(p, st);
+    return s.split == 8 ? launch<T, 8>(p, s, st) : s.split == 4 ? launch<T, 4>(p, s, st) : s.split == 2 ? launch<T, 2>(p, s, st) : launch<T, 1>(p, s, st);
 }
 
 }  // namespace
 
-cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, int split, cudaStream_t st)
+cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st)
 {
-    if (split == 0) {
-        // As many CTAs as ask for the weights faster than fewer would; clusters of eight that have their SMs to themselves find room for a few only.
-        // us at 1 / 32 / 64 / 128 rows with 2, 4, 8 CTAs a tile: N = K = 4096 (32 tiles) 6.0 6.4 6.9 8.2, 5.4 6.0 6.7 8.1, 5.4 6.4 7.9 19;
-        // N = 1024, K = 4096 (8 tiles) 5.0 5.4 5.9 7.2, 3.9 4.3 4.8 6.2, 3.4 4.0 4.7 6.0; N = 2048, K = 8192 (16) 8.6 9.0 9.7 11.7, 5.8 6.3 6.9 8.3, 5.5
-        // 6.2 11.3 14.2; N = 5003, K = 2011 (40) 5.2 5.8 5.8 7.5, 4.3 5.1 6.6 12.7, 7.2 8.5 10.4 14.6; N = 16 384 (128) one 13.7, two 13.7, four 15.4.
-        const int KB = (p.K - 1) / BK + 1, sms = qvggt_sm_count();
-        const long long tiles = ((p.N - 1) / CH + 1) * (long long)((p.M - 1) / MAX_TOK + 1);
-        for (split = tiles <= sms / 16 ? MAX_SPLIT : 4; split > 1 && (tiles * split > (p.M <= 32 ? sms + sms / 4 : sms) || KB < 2 * split); split /= 2) {}
-    }
-    if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, split, st);
-    return p.type == QVGGT_FP16 ? by_split<__half>(p, split, st) : by_split<float>(p, split, st);
+    if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, plan, st);
+    return p.type == QVGGT_FP16 ? by_split<__half>(p, plan, st) : by_split<float>(p, plan, st);
 }
 
 cudaError_t qvggt_read_split_status(int *code) { return cudaMemcpyFromSymbol(code, split_status, sizeof(int)); }

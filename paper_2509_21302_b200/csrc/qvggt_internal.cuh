@@ -117,8 +117,8 @@ struct QvggtLinear {
 };
 cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st);      // linear_few.cu
 cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st);    // gemm_c8.cu; cudaErrorNotSupported: sizes beyond its plan
-// linear_split.cu; split: CTAs that share the K of a tile (1, 2, 4, 8; 0: as suits the sizes)
-cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, int split, cudaStream_t st);
+namespace linear_plan { struct Split; }
+cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st);     // linear_split.cu
 cudaError_t qvggt_read_split_status(int *code);
 cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st);          // linear_few.cu: the one that suits the sizes
 cudaError_t qvggt_read_linear_status(int *code);                                 // the current device's status word of the launches without a handle
