@@ -531,8 +531,9 @@ def _vector(t: torch.Tensor, n: int, dtype: torch.dtype = torch.float32) -> int:
 
 def _new_rows(M: int, K: int, dtype: torch.dtype, device) -> torch.Tensor:
     """Rows a multiple of 16 bytes apart (a view, where K elements are no such multiple): as linear_c8 reads codes, and as they are written
-    fastest."""
-    step = 16 // dtype.itemsize
+    fastest.  Codes of more than 128: a multiple of 128 bytes, which the product's loads are made of (31 228 x 618 by 1152 channels: 34 us with
+    rows 16 bytes apart, 27 with 128)."""
+    step = 128 if dtype == torch.int8 and K > 128 else 16 // dtype.itemsize
     return torch.empty((M, (K + step - 1) // step * step), dtype=dtype, device=device)[:, :K]
 
 

@@ -398,11 +398,11 @@ struct Plain {
         return t;
     }
     static int64_t ld(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : up(t.size(1), 16); }
-    // `given`, or a new matrix whose rows are a multiple of 16 bytes apart.
+    // `given`, or a new matrix whose rows are as far apart as _new_rows() of binding.py makes them.
     static Tensor or_new(const Tensor &given, int64_t M, int64_t K, const at::TensorOptions &options, ScalarType type)
     {
         if (given.defined()) return given;
-        const int64_t width = up(K, 16 / static_cast<int64_t>(c10::elementSize(type)));
+        const int64_t width = up(K, type == at::kChar && K > 128 ? 128 : 16 / static_cast<int64_t>(c10::elementSize(type)));
         const Tensor t = at::empty({M, width}, options.dtype(type));
         return width == K ? t : t.as_strided({M, K}, {width, 1});
     }

@@ -90,13 +90,13 @@ __device__ int linear_status;          // the status word of the launches withou
 
 // 16 rows x 64 channels as 16x256b fragments (see gemmc::finish_16x64_tma): fma(float(acc), fl(a_scale * w_scale), bias) in T, staged in the
 // warp's 2 KB (`stg`; 128-byte swizzle) and stored: by TMA, or by ordinary stores of neighbouring elements, rows from Y on with
-// stride ldy, of which `rows` x `cols` exist.  Ordinary stores take the ROWS forms and the piece that N ends in where N elements are no
-// multiple of 16 bytes: a TMA store writes whole 16 bytes there, over what lies behind the row.  fp32 takes two stages of 32 channels each,
-// 2 KB apart where stg_next is not 0.
+// stride ldy, of which `rows` x `cols` exist.  Ordinary stores take the ROWS forms, and the last `tail` elements of a row that are no whole 16
+// bytes: a TMA store would write all 16, over what lies behind the row (the whole piece that N ends in by ordinary stores: N = 618, K = 618, 64
+// rows 5.0 us).  fp32 takes two stages of 32 channels each, 2 KB apart where stg_next is not 0.
 template <class T, bool ROWS>
 __device__ __forceinline__ void finish_16x64_any(const uint32_t (&raw)[32], const uint64_t (&as2)[2], const uint64_t (&w2)[8], const uint32_t (&c0)[8], const uint32_t (&c1)[8],
                                                  unsigned char *stg, uint32_t stg_addr, uint32_t stg_next, bool reused, const void *map_y, int x, int y, bool issue, int lane, uint64_t policy,
-                                                 T *Y, long long ldy, int rows, int cols)
+                                                 T *Y, long long ldy, int rows, int cols, int tail)
 {
     constexpr int HALVES = sizeof(T) == 4 ? 2 : 1, COLS = 64 / HALVES;
     const int t = lane & 3;
@@ -120,7 +120,6 @@ __device__ __forceinline__ void finish_16x64_any(const uint32_t (&raw)[32], cons
         }
         const uint32_t at = half * stg_next;
         const int left = cols - half * COLS;
-        const bool ordinary = ROWS || (left < COLS && left * (int)sizeof(T) % 16 != 0);
         if ((reused || (half && !stg_next)) && !ROWS && lane == 0) ptx::tma_store_wait_read<0>();
         __syncwarp();                       // the previous rows have left the staging tile
         if constexpr (sizeof(T) == 2) {
@@ -138,23 +137,32 @@ __device__ __forceinline__ void finish_16x64_any(const uint32_t (&raw)[32], cons
                     *reinterpret_cast<float2 *>(stg + at + r * 128 + (((2 * i + (t >> 1)) ^ (r & 7)) << 4) + 8 * (t & 1)) = make_float2(z[i][h][0], z[i][h][1]);
                 }
         }
-        if (ordinary) {
+        auto staged = [&](int r, int c) {
+            const int byte = c * (int)sizeof(T);
+            return *reinterpret_cast<const T *>(stg + at + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+        };
+        if constexpr (ROWS) {
             __syncwarp();
 #pragma unroll
             for (int r = 0; r < 16; ++r)
 #pragma unroll
                 for (int k = 0; k < COLS / 32; ++k) {
-                    const int c = lane + 32 * k, byte = c * (int)sizeof(T);
-                    const T v = *reinterpret_cast<const T *>(stg + at + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+                    const int c = lane + 32 * k;
+                    const T v = staged(r, c);
                     if (r < rows && c < left) Y[r * ldy + half * COLS + c] = v;
                 }
             __syncwarp();
         } else {
             ptx::fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0 && issue && left > 0) {
+            if (lane == 0 && issue && left > tail) {
                 ptx::tma_store_2d(map_y, stg_addr + at, x + half * COLS, y, policy);
                 ptx::tma_store_commit();
+            }
+            if (tail && left > 0 && left <= COLS) {              // two lanes a row
+                const int r = lane >> 1;
+                for (int c = left - tail + (lane & 1); c < left && r < rows; c += 2) Y[r * ldy + half * COLS + c] = staged(r, c);
+                __syncwarp();
             }
         }
     }
@@ -306,7 +314,7 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                             } else {
                                 const uint32_t at = stg + (PIECES / 2 * k + PIECES / 4 * u) * stg_next;
                                 finish_16x64_any<T, ROWS>(raw[u], as2[u], w2[k], c2[k], c2_more[k], smem + (at - sbase), at, stg_next, !last, &map_y, n, m, m < M, lane, policy,
-                                                          static_cast<T *>(Y) + (long long)m * ldy + n, ldy, M - m, N - n);
+                                                          static_cast<T *>(Y) + (long long)m * ldy + n, ldy, M - m, N - n, N % (16 / (int)sizeof(T)));
                             }
                             if (DUMP && acc_debug) gemmc::dump_16x64<0>(acc_debug + (long long)m * N + n, N, raw[u], M - m, lane);
                         }
@@ -727,7 +735,7 @@ cudaError_t launch_plan(const Call &c, cudaStream_t st)
     if (!qvggt_make_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.x, c.K, c.M, c.ldx, BK, BM, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !qvggt_make_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.w, c.K, c.N, c.ldw, BK, plan.wide * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
         !qvggt_make_map(&map_wu, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.w, c.K, c.N, c.ldw, BK, plan.cut * (UNIT / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
-        (FORM >= ROWS_BF16 ? false : !qvggt_make_map(&map_y, y_type, c.Y, c.N, c.M, (uint64_t)c.ldy * sizeof(T), 128 / sizeof(T), 16, CU_TENSOR_MAP_SWIZZLE_128B)))
+        (FORM >= ROWS_BF16 ? false : !qvggt_make_map(&map_y, y_type, c.Y, c.N - c.N % (16 / sizeof(T)), c.M, (uint64_t)c.ldy * sizeof(T), 128 / sizeof(T), 16, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorInvalidValue;
     if (FORM >= ROWS_BF16) map_y = map_x;                 // prefetched, not used
     cudaLaunchAttribute attr[2];
@@ -831,7 +839,8 @@ cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st)
 {
     if (!can_plan(p.M, p.N)) return cudaErrorNotSupported;
     const Call c = {p.Xq8, p.Wq8, p.ldx, p.ldw, p.a_scale, p.w_scale, p.bias, p.M, p.N, p.K, p.Y, p.ldy, nullptr, nullptr, ptx::kWaitLimitCycles, 0};
-    const bool tma = (reinterpret_cast<uintptr_t>(p.Y) & 15u) == 0 && p.ldy * (p.type == QVGGT_FP32 ? 4 : 2) % 16 == 0;
+    const int e = p.type == QVGGT_FP32 ? 4 : 2;
+    const bool tma = (reinterpret_cast<uintptr_t>(p.Y) & 15u) == 0 && p.ldy * e % 16 == 0 && (long long)p.N * e >= 16;
     if (p.type == QVGGT_BF16) return tma ? launch_form<false, FORM_BF16>(c, st) : launch_form<false, ROWS_BF16>(c, st);
     if (p.type == QVGGT_FP16) return tma ? launch_form<false, FORM_FP16>(c, st) : launch_form<false, ROWS_FP16>(c, st);
     return tma ? launch_form<false, FORM_FP32>(c, st) : launch_form<false, ROWS_FP32>(c, st);
