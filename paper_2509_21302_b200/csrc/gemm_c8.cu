@@ -181,7 +181,9 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 {
     using T = typename ResultType<FORM>::T;
     constexpr bool ROWS = FORM >= ROWS_BF16;
-    const uint16_t *__restrict__ bias = static_cast<const uint16_t *>(bias_);      // (HANDLE)
+    const uint16_t *__restrict__ bias = static_cast<const uint16_t *>(bias_);      // (of 16 bits)
+    // whether two channels' parameters can be read at once
+    const bool wide = ((reinterpret_cast<uintptr_t>(w_scale) & 7) | (reinterpret_cast<uintptr_t>(bias_) & (2 * sizeof(T) - 1))) == 0;
     int *status = FORM == HANDLE ? status_ : &linear_status;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -257,9 +259,15 @@ gemm_c8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int n = n0 + (k < units ? k * UNIT : 0) + 8 * e + 2 * (lane & 3);
-                    if constexpr (FORM == HANDLE) {
+                    if (FORM == HANDLE || (wide && n0 + units * UNIT <= N)) {
                         w2[k][e] = __ldg(reinterpret_cast<const unsigned long long *>(w_scale + n));
-                        c2[k][e] = bias ? __ldg(reinterpret_cast<const uint32_t *>(bias + n)) : 0u;
+                        if constexpr (sizeof(T) == 4) {
+                            const uint64_t c = bias_ ? __ldg(reinterpret_cast<const unsigned long long *>(static_cast<const float *>(bias_) + n)) : 0ull;
+                            c2[k][e] = static_cast<uint32_t>(c);
+                            c2_more[k][e] = static_cast<uint32_t>(c >> 32);
+                        } else {
+                            c2[k][e] = bias ? __ldg(reinterpret_cast<const uint32_t *>(bias + n)) : 0u;
+                        }
                     } else {                                       // off wide boundaries and up to N, where nothing is read
                         w2[k][e] = ptx::f32x2_pack(n < N ? __ldg(w_scale + n) : 0.0f, n + 1 < N ? __ldg(w_scale + n + 1) : 0.0f);
                         const T *b = static_cast<const T *>(bias_);
