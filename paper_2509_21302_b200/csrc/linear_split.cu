@@ -24,6 +24,9 @@ using linear_plan::CH;                 // channels of a tile: rows of the MMA, T
 using linear_plan::MAX_TOK;            // tokens of a tile: columns of the MMA
 constexpr int WARPS = 8;
 constexpr int MAX_STAGES = 12;
+constexpr int AHEAD = 16;              // blocks brought into L2 before the previous kernel ends.  One row, us with 0 / 8 / 16 / 32 / all: N = K = 4096 5.8 /
+                                       // 5.4 / 5.4 / 5.4 / 5.4, N = 16 384, K = 4096 13.5 / 12.6 / 12.2 / 13.5 / 13.5, N = K = 7183 12.9 / 12.6 / 12.2 / 13.1 / 13.2,
+                                       // N = K = 16 384 43.8 / 42.7 / 42.9 / 44.5 / 52.6 (what comes too early is displaced again)
 static_assert(CH == 128 && BK == 128 && MAX_TOK == 256, "what the instruction descriptor and tensor memory take");
 constexpr int W_BYTES = CH * BK;
 constexpr int OFF_FULL = 0, OFF_EMPTY = OFF_FULL + 8 * MAX_STAGES, OFF_DONE = OFF_EMPTY + 8 * MAX_STAGES, OFF_TMEM = OFF_DONE + 8, OFF_ABORT = OFF_TMEM + 4;
@@ -71,11 +74,11 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *s_tmem;
-    // The next kernel of the stream may set itself up, and the weights may be on their way to L2, while the previous one ends: a prefetch
-    // neither sees nor changes what that may still write.
+    // The next kernel of the stream may set itself up, and the first weights may be on their way to L2, while the previous one ends: a
+    // prefetch neither sees nor changes what that may still write.
     ptx::grid_launch_dependents();
     if (warp == 0 && ptx::elect_one())
-        for (int i = 0; i < blocks; ++i) ptx::tma_prefetch_2d(&map_w, (first + i) * BK, n0);
+        for (int i = 0; i < min(blocks, AHEAD); ++i) ptx::tma_prefetch_2d(&map_w, (first + i) * BK, n0);
     __syncwarp();
     ptx::grid_dependency_wait();
 
