@@ -271,6 +271,8 @@ int qvggt_gelu(const void *X_bf16, long long ldx, int M, int K, void *Y_bf16, vo
  * from a rotated handle -- RMS norms, other widths, weights quantized elsewhere.  Rows of any length K from 1 to 131056, rows of any
  * leading dimension from K on; activations, residual, results and bias are of one of three types; all arithmetic is fp32.
  *
+ * Outputs must not overlap inputs, except as qvggt_rmsnorm allows.
+ *
  * Per row:  amax = max(max_k |y[k]|, 1e-8),  scale = amax / 127,  q[k] = round(y[k] * (127 * (1 / amax))), codes in [-127, 127]
  * (every operation rounded to fp32 by itself, then half to even).
  * A row that holds a NaN or an infinity gets the scale NaN and codes 0, so that every result computed from it is NaN.
@@ -303,7 +305,10 @@ int qvggt_dequantize_c8(const signed char *Xq8, long long ldq, const float *a_sc
 int qvggt_rmsnorm(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K, const float *gamma,
                   float eps, void *H, long long ldh, void *Y, long long ldy, void *cuda_stream);
 
-/* The same norm with its output in 8 bits: the unrounded y goes straight into the quantizer and never to memory. */
+/*
+ * The same norm with its output in 8 bits: the unrounded y goes straight into the quantizer and never to memory.  (rstd is common to a row, so
+ * its codes are taken from h * gamma, which has to be within fp32's range, and rstd goes into the scale.)  H may be X or residual itself.
+ */
 int qvggt_rmsnorm_quantize_c8(const void *X, const void *residual, int type, long long ldx, long long ldr, int M, int K,
                               const float *gamma, float eps, void *H, long long ldh, signed char *Xq8, long long ldq, float *a_scale,
                               void *cuda_stream);
@@ -327,6 +332,16 @@ int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale,
  * positive code of the first wait that gave up (the results of that call are not all written), and QVGGT_ERR_DEVICE_TIMEOUT.
  */
 int qvggt_linear_status(void *cuda_stream, int *code);
+
+/*
+ * Test hook for the bounded waits of qvggt_linear_c8's split kernel, as qvggt_debug_starved_linear_c8 for the handles' GEMM: the launch without
+ * its loads, every wait limited to wait_limit_cycles (1000 .. 2e9, exclusive) SM cycles.  The first wait runs out, the kernel records its code in
+ * the device's status word (sticky: qvggt_linear_status reports it from then on), releases its tensor memory and returns.  M from 1 to 512;
+ * what is in Y afterwards is not defined.
+ */
+int qvggt_debug_starved_linear(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw,
+                               const float *w_scale, int M, int N, int K, void *Y_bf16, long long ldy, long long wait_limit_cycles,
+                               void *cuda_stream);
 
 /* Frees the handle and its device memory (synchronises the device first).  At most 64 MB per device stay with the library for
  * the next handle; they go back to the driver when an allocation of the library fails.  NULL is allowed. */

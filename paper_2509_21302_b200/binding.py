@@ -32,7 +32,7 @@ EXPORTS = ("qvggt_prepare_weights", "qvggt_rotate_smooth_quantize", "qvggt_w4a4_
            "qvggt_rotate_smooth_quantize_c8_grouped", "qvggt_w4a4_linear_c8_grouped",
            "qvggt_rotate_smooth_quantize_c8_expand", "qvggt_w4a4_linear_c8_expanded",
            "qvggt_quantize_c8", "qvggt_dequantize_c8", "qvggt_rmsnorm", "qvggt_rmsnorm_quantize_c8", "qvggt_linear_c8",
-           "qvggt_linear_status")
+           "qvggt_linear_status", "qvggt_debug_starved_linear")
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # QVGGT_BF16, QVGGT_FP16, QVGGT_FP32
 PREP_C8 = 1   # QVGGT_PREP_C8: keep an int8 [N, K] copy of the weight codes for the *_c8 entry points
 PREP_W8A8 = 2  # QVGGT_PREP_W8A8: 8-bit codes (one per byte only)
@@ -92,6 +92,7 @@ def lib() -> ctypes.CDLL:
         L.qvggt_rmsnorm.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp]
         L.qvggt_rmsnorm_quantize_c8.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, f32, vp, i64, vp, i64, vp, vp]
         L.qvggt_linear_c8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
+        L.qvggt_debug_starved_linear.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, i64, i64, vp]
         L.qvggt_linear_status.argtypes = [vp, ctypes.POINTER(i32)]
         L.qvggt_status_string.argtypes = [i32]
         L.qvggt_status_string.restype = ctypes.c_char_p
@@ -646,3 +647,11 @@ def linear_status() -> int:
     if st not in (OK, -6):
         raise QvggtError(st, "qvggt_linear_status")
     return code.value
+
+
+def debug_starved_linear(Xq8: torch.Tensor, a_scale: torch.Tensor, Wq8: torch.Tensor, w_scale: torch.Tensor, Y: torch.Tensor, wait_limit_cycles: int) -> int:
+    """Test hook: linear_c8's split kernel with its loads switched off and short wait limits; returns the C status of the launch (the expired
+    wait shows in linear_status(), for the rest of the process)."""
+    (M, K), N = Xq8.shape, Wq8.shape[0]
+    return lib().qvggt_debug_starved_linear(_ptr(Xq8), _rows(Xq8, M, K, torch.int8), _vector(a_scale, M), _ptr(Wq8), _rows(Wq8, N, K, torch.int8), _vector(w_scale, N),
+                                            M, N, K, _ptr(Y), _rows(Y, M, N, torch.bfloat16), wait_limit_cycles, _stream())

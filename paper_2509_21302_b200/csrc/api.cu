@@ -449,8 +449,9 @@ int qvggt_rmsnorm_quantize_c8(const void *X, const void *residual, int type, lon
     return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
 }
 
-int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw, const float *w_scale,
-                    const void *bias, int M, int N, int K, void *Y, int type, long long ldy, void *cuda_stream)
+// Checks the arguments of qvggt_linear_c8; QVGGT_OK with *p filled in, or (M = 0) with p->M = 0.
+static int check_linear(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw, const float *w_scale,
+                        const void *bias, int M, int N, int K, void *Y, int type, long long ldy, QvggtLinear *p)
 {
     if (!valid_type(type)) return QVGGT_ERR_UNSUPPORTED;
     if (M < 0 || M > MAX_ROWS || N < 1 || K < 1 || K > MAX_ROW) return QVGGT_ERR_SHAPE;
@@ -461,10 +462,29 @@ int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale,
         !element_aligned(bias, type) || !element_aligned(Y, type))
         return QVGGT_ERR_ALIGN;
     if (!device_is_sm100()) return QVGGT_ERR_UNSUPPORTED;
+    p->Xq8 = Xq8; p->Wq8 = Wq8; p->ldx = ldx; p->ldw = ldw; p->ldy = ldy; p->a_scale = a_scale; p->w_scale = w_scale; p->bias = bias; p->Y = Y;
+    p->M = M; p->N = N; p->K = K; p->type = type;
+    return QVGGT_OK;
+}
+
+int qvggt_linear_c8(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw, const float *w_scale,
+                    const void *bias, int M, int N, int K, void *Y, int type, long long ldy, void *cuda_stream)
+{
     QvggtLinear p = {};
-    p.Xq8 = Xq8; p.Wq8 = Wq8; p.ldx = ldx; p.ldw = ldw; p.ldy = ldy; p.a_scale = a_scale; p.w_scale = w_scale; p.bias = bias; p.Y = Y;
-    p.M = M; p.N = N; p.K = K; p.type = type;
+    const int bad = check_linear(Xq8, ldx, a_scale, Wq8, ldw, w_scale, bias, M, N, K, Y, type, ldy, &p);
+    if (bad != QVGGT_OK || M == 0) return bad;
     cudaError_t e = qvggt_launch_linear(p, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
+}
+
+int qvggt_debug_starved_linear(const signed char *Xq8, long long ldx, const float *a_scale, const signed char *Wq8, long long ldw, const float *w_scale,
+                               int M, int N, int K, void *Y_bf16, long long ldy, long long wait_limit_cycles, void *cuda_stream)
+{
+    if (M < 1 || M > 512 || wait_limit_cycles < 1000 || wait_limit_cycles >= 2000000000LL) return QVGGT_ERR_SHAPE;
+    QvggtLinear p = {};
+    const int bad = check_linear(Xq8, ldx, a_scale, Wq8, ldw, w_scale, nullptr, M, N, K, Y_bf16, QVGGT_BF16, ldy, &p);
+    if (bad != QVGGT_OK) return bad;
+    cudaError_t e = qvggt_launch_linear_starved(p, wait_limit_cycles, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? QVGGT_OK : QVGGT_ERR_CUDA;
 }
 

@@ -41,13 +41,16 @@ __device__ __forceinline__ uint4 ld_cluster(uint32_t addr)
     return v;
 }
 
+// wait_limit: bound of every device-side wait, in cycles; any but the usual one starves the kernel: nothing is loaded, so that the first wait for
+// operands runs out (used only to exercise that path; no asynchronous operation is in flight).
 // One tile of CH channels x tok tokens per cluster of SPLIT CTAs; blockIdx.x = tile * SPLIT + rank, blockIdx.y = tile of tokens.
 template <class T, int SPLIT>
 __global__ void __launch_bounds__(WARPS * 32)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const float *__restrict__ a_scale, const float *__restrict__ w_scale,
-                    const T *__restrict__ bias, T *__restrict__ Y, long long ldy, int M, int N, int K, int tok, int stages, int tmem_cols)
+                    const T *__restrict__ bias, T *__restrict__ Y, long long ldy, int M, int N, int K, int tok, int stages, int tmem_cols, long long wait_limit)
 {
     int *status = &split_status;
+    const bool starved = wait_limit != ptx::kWaitLimitCycles;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sbase = ptx::smem_addr(smem), ops = sbase + OFF_OPS;
@@ -77,24 +80,24 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     // The next kernel of the stream may set itself up, and the first weights may be on their way to L2, while the previous one ends: a
     // prefetch neither sees nor changes what that may still write.
     ptx::grid_launch_dependents();
-    if (warp == 0 && ptx::elect_one())
+    if (warp == 0 && !starved && ptx::elect_one())
         for (int i = 0; i < min(blocks, AHEAD); ++i) ptx::tma_prefetch_2d(&map_w, (first + i) * BK, n0);
     __syncwarp();
     ptx::grid_dependency_wait();
 
     if (warp == 0) {
-        if (ptx::elect_one()) {
+        if (!starved && ptx::elect_one()) {
             gemmc::Ring r;
             int i = 0;
             for (; i < blocks; ++i) {
-                if (i >= stages && !ptx::mbar_wait(bar_empty + 8 * r.s, r.ph ^ 1, s_abort, status, QVGGT_DEV_TIMEOUT_EMPTY)) break;
+                if (i >= stages && !ptx::mbar_wait(bar_empty + 8 * r.s, r.ph ^ 1, s_abort, status, QVGGT_DEV_TIMEOUT_EMPTY, 0, wait_limit)) break;
                 const uint32_t stage = ops + r.s * stage_bytes;
                 ptx::mbar_arrive_expect_tx(bar_full + 8 * r.s, stage_bytes);
                 ptx::tma_load_2d(&map_w, bar_full + 8 * r.s, stage, (first + i) * BK, n0);
                 ptx::tma_load_2d(&map_x, bar_full + 8 * r.s, stage + W_BYTES, (first + i) * BK, m0);
                 r.advance(stages);
             }
-            if (!ptx::mbar_wait(bar_done, 0, s_abort, status, QVGGT_DEV_TIMEOUT_ACCUM, 20))       // the copies in flight end before the CTA does
+            if (!ptx::mbar_wait(bar_done, 0, s_abort, status, QVGGT_DEV_TIMEOUT_ACCUM, 20, wait_limit))       // the copies in flight end before the CTA does
                 for (int j = max(0, i - stages); j < i; ++j)
                     for (int n = 0; n < 100000 && !ptx::mbar_try_wait(bar_full + 8 * (j % stages), (j / stages) & 1); ++n) {}
         }
@@ -104,7 +107,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             const uint32_t idesc = ptx::idesc_i8(CH, tok);
             gemmc::Ring r;
             for (int i = 0; i < blocks; ++i) {
-                if (!ptx::mbar_wait(bar_full + 8 * r.s, r.ph, s_abort, status, QVGGT_DEV_TIMEOUT_FULL)) break;
+                if (!ptx::mbar_wait(bar_full + 8 * r.s, r.ph, s_abort, status, QVGGT_DEV_TIMEOUT_FULL, 0, wait_limit)) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t stage = ops + r.s * stage_bytes;
                 gemmc::mma_kblock_i8<false>(tmem, stage, stage + W_BYTES, idesc, i == 0);
@@ -118,7 +121,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 
     // Partial sums to shared memory, over the operands: behind the last MMA nothing reads them, and every load has been consumed by one.
     int *part = reinterpret_cast<int *>(smem + OFF_OPS);
-    bool alive = ptx::mbar_wait(bar_done, 0, s_abort, status, QVGGT_DEV_TIMEOUT_ACCUM, 20);
+    bool alive = ptx::mbar_wait(bar_done, 0, s_abort, status, QVGGT_DEV_TIMEOUT_ACCUM, 20, wait_limit);
     alive = __all_sync(0xFFFFFFFFu, alive);
     ptx::tc_fence_after_sync();
     if (alive) {
@@ -196,7 +199,7 @@ constexpr int SMEM_FULL = 232448 - 2048;      // stages of a CTA that has its SM
 constexpr int SMEM_HALF = 232448 / 2 - 4096;
 
 template <class T, int SPLIT>
-cudaError_t launch(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st)
+cudaError_t launch(const QvggtLinear &p, const linear_plan::Split &plan, long long wait_limit, cudaStream_t st)
 {
     static QvggtPerDevice cache;
     int sms = 0;
@@ -233,21 +236,27 @@ cudaError_t launch(const QvggtLinear &p, const linear_plan::Split &plan, cudaStr
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, linear_split_kernel<T, SPLIT>, map_w, map_x, p.a_scale, p.w_scale, static_cast<const T *>(p.bias), static_cast<T *>(p.Y), p.ldy,
-                              p.M, p.N, p.K, tok, stages, tmem_cols);
+                              p.M, p.N, p.K, tok, stages, tmem_cols, wait_limit);
 }
 
 template <class T>
-cudaError_t by_split(const QvggtLinear &p, const linear_plan::Split &s, cudaStream_t st)
+cudaError_t by_split(const QvggtLinear &p, const linear_plan::Split &s, long long limit, cudaStream_t st)
 {
-    return s.split == 8 ? launch<T, 8>(p, s, st) : s.split == 4 ? launch<T, 4>(p, s, st) : s.split == 2 ? launch<T, 2>(p, s, st) : launch<T, 1>(p, s, st);
+    return s.split == 8 ? launch<T, 8>(p, s, limit, st) : s.split == 4 ? launch<T, 4>(p, s, limit, st) : s.split == 2 ? launch<T, 2>(p, s, limit, st) : launch<T, 1>(p, s, limit, st);
 }
 
 }  // namespace
 
 cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st)
 {
-    if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, plan, st);
-    return p.type == QVGGT_FP16 ? by_split<__half>(p, plan, st) : by_split<float>(p, plan, st);
+    if (p.type == QVGGT_BF16) return by_split<__nv_bfloat16>(p, plan, ptx::kWaitLimitCycles, st);
+    return p.type == QVGGT_FP16 ? by_split<__half>(p, plan, ptx::kWaitLimitCycles, st) : by_split<float>(p, plan, ptx::kWaitLimitCycles, st);
+}
+
+cudaError_t qvggt_launch_linear_starved(const QvggtLinear &p, long long wait_limit_cycles, cudaStream_t st)
+{
+    const int sms = qvggt_sm_count();
+    return sms < 1 ? cudaErrorInvalidDevice : by_split<__nv_bfloat16>(p, linear_plan::best_split(p.M, p.N, p.K, sms), wait_limit_cycles, st);
 }
 
 cudaError_t qvggt_read_split_status(int *code) { return cudaMemcpyFromSymbol(code, split_status, sizeof(int)); }

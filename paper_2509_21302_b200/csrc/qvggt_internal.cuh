@@ -119,6 +119,8 @@ cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st);     
 cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st);    // gemm_c8.cu; cudaErrorNotSupported: sizes beyond its plan
 namespace linear_plan { struct Split; }
 cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st);     // linear_split.cu
+// The same launch (bf16 results) without its loads and with a short wait limit: the first wait for operands runs out.
+cudaError_t qvggt_launch_linear_starved(const QvggtLinear &p, long long wait_limit_cycles, cudaStream_t st);
 cudaError_t qvggt_read_split_status(int *code);
 cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st);          // linear_few.cu: the one that suits the sizes
 cudaError_t qvggt_read_linear_status(int *code);                                 // the current device's status word of the launches without a handle

@@ -83,3 +83,11 @@ def test_the_binding_refuses_host_tensors():
                  lambda: q.linear_c8(xq, a, w, torch.ones(32))):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_the_starved_launch_is_bounded():
+    def starved(M=4, limit=100000, Xq=FAKE):
+        return q.lib().qvggt_debug_starved_linear(Xq, 64, FAKE, FAKE, 64, FAKE, M, 32, 64, FAKE, 32, limit, None)
+
+    assert starved(M=0) == SHAPE and starved(M=513) == SHAPE and starved(limit=999) == SHAPE and starved(limit=2000000000) == SHAPE
+    assert starved(Xq=None) == NULL and starved(Xq=FAKE + 8) == ALIGN
