@@ -4,10 +4,10 @@
 //   y[k] = (h[k] * rstd) * gamma[k],  rstd = 1 / sqrt(sum h^2 / K + eps)
 //   amax = max(max_k |y[k]|, 1e-8),  scale = amax / 127,  q[k] = round(y[k] * (127 * (1 / amax))), half to even
 // In the quantizer every one of these operations is rounded to fp32 by itself, so that its codes are those of the formula in plain fp32
-// arithmetic, bit for bit.  That shows where elements of 16 bits lie exactly between two codes: with the product rounded straight to the
+// arithmetic, bit for bit (behind the norm they are taken from h gamma, see Row).  That shows where elements of 16 bits lie exactly between two codes: with the product rounded straight to the
 // integer (one multiply-add) other codes came out there.
 // They move K e bytes in, K (and K e) out, against a handful of operations per element: HBM bounds them from a few hundred rows on,
-// and latency (one load, two reductions, one store) below.  A row therefore stays in registers between its one load and its one store.
+// and latency (one load, one reduction, one store) below.  A row therefore stays in registers between its one load and its one store.
 #include "element.cuh"
 #include "gemm_common.cuh"
 #include "qvggt_internal.cuh"
@@ -131,7 +131,7 @@ struct Row {
         if (NORM) rstd = rsqrtf(__fmaf_rn(sum, p.one_over_k, p.eps));
         if (QUANT) {
             const float t = __uint_as_float(top), amax = NORM ? __fmul_rn(t, rstd) : t;
-            finite = top < 0x7F800000u && !(amax != amax);
+            finite = top < 0x7F800000u && amax < __uint_as_float(0x7F800000u);       // neither infinite nor NaN
             const float f = amax >= 1e-8f ? __fmul_rn(__frcp_rn(t), 127.0f) : __fmul_rn(p.floor_factor, rstd);
             factor = ptx::f32x2_pack(f, f);
             if (scale) *scale = finite ? __fdiv_rn(fmaxf(amax, 1e-8f), 127.0f) : __uint_as_float(0x7FC00000u);

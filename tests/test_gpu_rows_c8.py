@@ -185,6 +185,22 @@ def test_rows_of_zeros_ties_and_non_finite_values(K, dtype):
     assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all()
 
 
+@pytest.mark.parametrize("K", [64, 100, 1024, 5000, 40000])
+def test_rows_at_the_ends_of_the_range(K):
+    """Sums of squares beyond fp32 give 0; rows that no epsilon holds up are not finite; the largest and smallest fp32 values quantize."""
+    x = torch.ones(5, K, device="cuda")
+    x[0], x[1], x[2], x[3] = 1e25, 0.0, 1e-30, 3e38
+    gamma = torch.ones(K, device="cuda")
+    assert not q.rmsnorm(x, gamma)[0].any()
+    codes, scale = q.rmsnorm_quantize_c8(x, gamma, 1e-6)
+    assert not codes[0].any() and scale[0] == scale[1] == torch.tensor(1e-8) / torch.tensor(127.0) and not codes[1].any()
+    assert torch.all(codes[4] == 127)
+    codes, scale = q.rmsnorm_quantize_c8(x, gamma, 0.0)             # 0 / 0, and 1e-30 / sqrt(1e-60), which is 0 in fp32
+    assert torch.isnan(scale[1]) and torch.isnan(scale[2]) and not codes[1:3].any() and torch.all(codes[4] == 127)
+    codes, scale = q.quantize_c8(x)
+    assert torch.all(codes[3] == 127) and torch.all(codes[0] == 127) and torch.isfinite(scale).all() and not codes[1:3].any()
+
+
 def test_empty_batches():
     for dtype in TYPES:
         x = torch.empty(0, 100, dtype=dtype, device="cuda")
