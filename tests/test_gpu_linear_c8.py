@@ -219,3 +219,51 @@ def test_a_layer(M, K, N, dtype):
     # rms (gamma adds 1.5), so each of the four quantized operands is off by less than 9 / 127 / sqrt(12) = 2.1 % of its rms: 4.1 % in all,
     # with the 16-bit roundings below 0.5 % each.
     assert (y.double() - want).norm() <= 0.05 * want.norm()
+
+
+@pytest.mark.parametrize("M", [1, 20, 90, 300, 1500])
+def test_what_the_call_before_wrote(M):
+    """Weights, activations and scales written by the calls directly in front of the product, new ones every time: a launch may set itself
+    up, and bring weights to L2, while the one before it still runs."""
+    N, K = 1100, 2048
+    g = torch.Generator(device="cuda").manual_seed(M)
+    Ws = [torch.randn(N, K, generator=g, device="cuda") for _ in range(6)]
+    Xs = [torch.randn(M, K, generator=g, device="cuda").bfloat16() for _ in range(6)]
+    want = []
+    for W, X in zip(Ws, Xs):
+        c, s = q.quantize_c8(W)
+        xq, a = q.quantize_c8(X)
+        torch.cuda.synchronize()
+        want.append(q.linear_c8(xq, a, c, s, dtype=torch.float32))
+        torch.cuda.synchronize()
+    c, s = q.quantize_c8(torch.zeros_like(Ws[0]))
+    xq, a = q.quantize_c8(torch.zeros_like(Xs[0]))
+    for _ in range(3):
+        got = []
+        for W, X in zip(Ws, Xs):
+            q.quantize_c8(X, xq, a)
+            q.quantize_c8(W, c, s)
+            got.append(q.linear_c8(xq, a, c, s, dtype=torch.float32))
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        got = []
+        for W, X in zip(Ws, Xs):
+            q.quantize_c8(W, c, s)
+            q.quantize_c8(X, xq, a)
+            got.append(q.linear_c8(xq, a, c, s, dtype=torch.float32))
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_sizes(seed):
+    import random
+    r = random.Random(seed)
+    for _ in range(25):
+        M = int(2 ** r.uniform(0, 11))
+        N, K = int(2 ** r.uniform(0, 13)), int(2 ** r.uniform(0, 13))
+        dtype = r.choice(TYPES)
+        p = _problem(M, N, K, dtype, r.random() < 0.5, r.randrange(1000), pad=16 * r.randrange(3))
+        pad = r.choice((0, 0, 1, 8))
+        y = torch.full((M + 1, N + pad), 5.0, dtype=dtype, device="cuda")
+        q.linear_c8(*p, Y=y[:M, :N])
+        _check(y[:M, :N].contiguous(), *p)
+        assert (y[M] == 5).all() and (y[:, N:] == 5).all(), (M, N, K, dtype, pad)

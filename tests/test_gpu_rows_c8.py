@@ -286,3 +286,24 @@ def test_refusals():
     with pytest.raises(q.QvggtError) as e:
         q.rmsnorm(x, g, -1.0)
     assert e.value.status == -4
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_sizes(seed):
+    import random
+    rng = random.Random(seed)
+    for _ in range(25):
+        M, K = int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 13.5))
+        dtype, pad, shift = rng.choice(TYPES), rng.choice((0, 1, 3, 8, 24)), rng.choice((0, 0, 1, 8))
+        x, r = _matrix(M, K, dtype, rng.randrange(1000), pad, shift), _matrix(M, K, dtype, rng.randrange(1000), rng.choice((0, pad)))
+        gamma = torch.rand(K, device="cuda") + 0.5
+        codes, scale = q.quantize_c8(x)
+        _check_codes(codes, scale, x.double(), 127 * 3.1 * U, 0.0)
+        h64, y64 = _norm64(x, r, gamma, 1e-6)
+        half, tiny = torch.finfo(dtype).eps / 2, torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+        y, h = q.rmsnorm(x, gamma, 1e-6, r)
+        assert torch.all((y.double() - y64).abs() <= (half + 2 * NORM_REL) * y64.abs() + tiny)
+        assert torch.all((h.double() - h64).abs() <= (half + 2 * U) * h64.abs() + tiny)
+        codes, scale, h2 = q.rmsnorm_quantize_c8(x, gamma, 1e-6, r)
+        _check_codes(codes, scale, y64, 127 * (2 * NORM_REL + 3.1 * U), NORM_REL)
+        assert torch.equal(h, h2)
