@@ -144,7 +144,8 @@ cudaError_t qvggt_launch_linear(const QvggtLinear &p, cudaStream_t st)
     linear_plan::Split split = {};
     const linear_plan::Kernel kernel = linear_plan::choose(p.M, p.N, p.K, sms, &split);
     cudaError_t e = cudaErrorNotSupported;
-    if (kernel == linear_plan::SPLIT) e = qvggt_launch_linear_split(p, split, st);
+    if (kernel == linear_plan::TOKEN) e = qvggt_launch_linear_token(p, st);
+    else if (kernel == linear_plan::SPLIT) e = qvggt_launch_linear_split(p, split, st);
     else if (kernel == linear_plan::TILES) e = qvggt_launch_linear_tiles(p, st);
     return e == cudaErrorNotSupported ? qvggt_launch_linear_few(p, st) : e;       // also for sizes beyond what the others count with
 }

@@ -60,9 +60,23 @@ inline Split best_split(int M, int N, int K, int sms)
     return best;
 }
 
-enum Kernel { FEW, SPLIT, TILES };
+enum Kernel { TOKEN, FEW, SPLIT, TILES };
 
-// The kernel for few rows (linear_few.cu) starts fastest, but its loads wait for registers: it has the smallest products.  The tiles kernel
+// The kernel for one to four rows (linear_token.cu) reads the weights with ordinary loads and multiplies without the tensor core: it starts fastest,
+// and is the slower one where its arithmetic shows.  us, token / the best of the others (weights from memory):
+//   1 row    N = K = 1024 1.5 / 2.7    K = 4096 2.1 / 3.4    N = K = 4096 3.8 / 5.4    7183 11.0 / 12.3    N = 16384, K = 4096 12.0 / 12.4
+//            N = K = 16384 53 / 44     N = 64, K = 16384 2.0 / 4.8
+//   2 rows   N = K = 1024 1.6 / 2.7    4096 4.0 / 5.4         5792 9.7 / 9.5    N = 16384, K = 4096 14.0 / 12.4
+//   4 rows   N = K = 1024 2.1 / 2.7    4096 4.4 / 5.4         5792 10.2 / 9.5   N = 64, K = 16384 4.8 / 4.8    N = 128, K = 131056 55 / 27
+// Many short rows leave its lanes idle: 1 row, K = 64, N = 8192 2.1 / 2.8, 16384 3.4 / 2.9; K = 512, N = 32768 6.1 / 5.7; K = 1024 6.7 / 7.5.
+inline bool token_wins(int M, int N, int K)
+{
+    if (M > 4 || (long long)N * K > (M == 1 ? 1 << 26 : 1 << 24) || (M > 2 && K > 16384)) return false;
+    return N <= 8192 || K >= 1024;
+}
+
+// The kernel for few rows (linear_few.cu) starts faster than the two on the tensor core's fifth generation, but its loads wait for registers, and
+// K is shared by 16 warps only (8 rows, N = 256: K = 2048 2.8, split 2.9; 4096 3.6, 3.2): it has the smallest products.  The tiles kernel
 // (gemm_c8.cu) takes about 0.2 us per K-block and round of its 256 x 256 tiles, hardly less for fewer rows, and half of the weights' way from
 // memory on top; the split kernel is for batches.  us,
 // few / split / tiles (weights from memory):
@@ -76,7 +90,8 @@ enum Kernel { FEW, SPLIT, TILES };
 //   N = 2048, K = 8192    1 row 10.2 / 5.5 / 16.3  64 22.3 / 6.9 / 14.5  256 64 / 10.0 / 14.6    512 - / 14.2 / 14.4
 inline Kernel choose(int M, int N, int K, int sms, Split *s)
 {
-    if (M <= 8 && (long long)N * K <= 1 << 21) return FEW;
+    if (token_wins(M, N, K)) return TOKEN;
+    if (M <= 8 && (long long)N * K <= 1 << 21 && K <= 2048) return FEW;
     if (M > 512) return TILES;
     *s = best_split(M, N, K, sms);
     const int KB = (K - 1) / BK + 1, pairs = sms > 1 ? sms / 2 : 1;

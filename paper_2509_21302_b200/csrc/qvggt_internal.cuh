@@ -116,6 +116,7 @@ struct QvggtLinear {
     int M, N, K, type;
 };
 cudaError_t qvggt_launch_linear_few(const QvggtLinear &p, cudaStream_t st);      // linear_few.cu
+cudaError_t qvggt_launch_linear_token(const QvggtLinear &p, cudaStream_t st);    // linear_token.cu; cudaErrorNotSupported: more than four rows
 cudaError_t qvggt_launch_linear_tiles(const QvggtLinear &p, cudaStream_t st);    // gemm_c8.cu; cudaErrorNotSupported: sizes beyond its plan
 namespace linear_plan { struct Split; }
 cudaError_t qvggt_launch_linear_split(const QvggtLinear &p, const linear_plan::Split &plan, cudaStream_t st);     // linear_split.cu

@@ -267,3 +267,16 @@ def test_random_sizes(seed):
         q.linear_c8(*p, Y=y[:M, :N])
         _check(y[:M, :N].contiguous(), *p)
         assert (y[M] == 5).all() and (y[:, N:] == 5).all(), (M, N, K, dtype, pad)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("N,K", [(1, 1), (3, 15), (2, 511), (5, 513), (7, 1025), (65, 2047), (1, 16385), (33, 131056), (4097, 1024), (8193, 1023), (8193, 1024), (1001, 2500)])
+def test_single_tokens(M, N, K):
+    """One to five rows where their warps share a row or do not, with extreme codes; the rows are those of a longer call bit for bit."""
+    for dtype in TYPES:
+        p = _problem(M, N, K, dtype, dtype != torch.float16, K + M, lo=-128)
+        y = q.linear_c8(*p, dtype=dtype)
+        _check(y, *p)
+        xq, a = torch.zeros(40, (K + 15) // 16 * 16, dtype=torch.int8, device="cuda"), torch.ones(40, device="cuda")
+        xq[7:7 + M, :K], a[7:7 + M] = p[0], p[1]
+        assert torch.equal(q.linear_c8(xq[:, :K], a, *p[2:], dtype=dtype)[7:7 + M], y)

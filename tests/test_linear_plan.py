@@ -34,10 +34,15 @@ int main()
     int M = 1, N = 2147483647, K = 131056, sms = 148;
     if (check(M, N, K, sms) || check(512, N, 1, sms) || check(1, 1, 1, sms)) return 1;
     Split s = {};
-    CHECK(choose(1, 1024, 1024, sms, &s) == FEW);
+    CHECK(choose(1, 1024, 1024, sms, &s) == TOKEN);
+    CHECK(choose(1, 4096, 16384, sms, &s) == TOKEN && choose(2, 4096, 16384, sms, &s) == SPLIT);
+    CHECK(choose(4, 4096, 4096, sms, &s) == TOKEN && choose(5, 4096, 4096, sms, &s) == SPLIT);
+    CHECK(choose(1, 200000, 64, sms, &s) == SPLIT);
+    CHECK(choose(8, 1024, 1024, sms, &s) == FEW);
+    CHECK(choose(8, 1, 131056, sms, &s) == SPLIT);
     CHECK(choose(16, 1024, 1024, sms, &s) == SPLIT);
     CHECK(choose(128, 1024, 1024, sms, &s) == TILES);
-    CHECK(choose(1, 4096, 4096, sms, &s) == SPLIT && s.split == 4);
+    CHECK(choose(8, 4096, 4096, sms, &s) == SPLIT && s.split == 4);
     CHECK(choose(64, 4096, 4096, sms, &s) == SPLIT);
     CHECK(choose(128, 16384, 4096, sms, &s) == TILES);
     CHECK(choose(256, 1024, 4096, sms, &s) == SPLIT && s.tok < 256);
