@@ -1,6 +1,11 @@
-// Which kernel takes a product of 8-bit codes, and how the split kernel (linear_split.cu) cuts it up: plain arithmetic on the host, with no
-// CUDA header, so that it can be compiled and checked by itself.
+// Which kernel takes a product of 8-bit codes, and how the split kernel (linear_split.cu) cuts it up: plain arithmetic, with no CUDA header, so
+// that it can be compiled and checked by itself.
 #pragma once
+#ifndef __CUDACC__
+#define __host__
+#define __device__
+#define __forceinline__ inline
+#endif
 
 namespace linear_plan {
 
@@ -8,6 +13,9 @@ constexpr int CH = 128;                // channels of a tile of the split kernel
 constexpr int BK = 128;                // codes along K of a block
 constexpr int MAX_TOK = 256;           // tokens of a tile, a multiple of 16
 constexpr int FEW_ROWS = 48;           // row tiles are not made smaller than this
+
+// Whether the four channels from n on (0 <= n < N) exist.  N goes up to 2^31 - 1, so n + 4 need not be an int.
+__host__ __device__ __forceinline__ bool four_channels(int n, int N) { return n <= N - 4; }
 
 struct Split {
     int split;                         // CTAs that share the K of a tile

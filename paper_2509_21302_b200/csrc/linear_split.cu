@@ -176,7 +176,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[i] = __fmaf_rn(static_cast<float>(s[i]), __fmul_rn(as[j], ws[i]), bs[i]);
                 T *y = Y + (long long)(m0 + r) * ldy + n;
-                if (n + 4 <= N && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(T) - 1)) == 0) {
+                if (linear_plan::four_channels(n, N) && (reinterpret_cast<uintptr_t>(y) & (4 * sizeof(T) - 1)) == 0) {
                     if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(y) = make_float4(z[0], z[1], z[2], z[3]);
                     else *reinterpret_cast<uint2 *>(y) = make_uint2(element::pack2<T>(z[0], z[1]), element::pack2<T>(z[2], z[3]));
                 } else {
