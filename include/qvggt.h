@@ -270,7 +270,8 @@ int qvggt_gelu(const void *X_bf16, long long ldx, int M, int K, void *Y_bf16, vo
 /*
  * The rotation-free 8-bit path: the paper's "naive" W8A8 arm (Tab. "efficiency", 8/8 naive) and any layer whose codes do not come
  * from a rotated handle -- RMS norms, other widths, weights quantized elsewhere.  Rows of any length K from 1 to 131056, rows of any
- * leading dimension from K on; activations, residual, results and bias are of one of three types; all arithmetic is fp32.
+ * leading dimension from K on; activations, residual, results and bias are of one of three types; all arithmetic is fp32.  A row's results do not
+ * depend on M, on the other rows, or on how rows are aligned: they are bit for bit those of the same row in a call of its own.
  *
  * Outputs must not overlap inputs, except as qvggt_rmsnorm allows.
  *

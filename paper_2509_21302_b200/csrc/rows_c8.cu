@@ -74,6 +74,32 @@ __device__ __forceinline__ void reduce_row(float &s, uint32_t &a, uint2 *part)
     if (MAX) a = __reduce_max_sync(0xFFFFFFFFu, a);
 }
 
+// The same where a warp stands for two (see rows_kernel): s is the sum of the first, `more` that of the second, as many warps further on.  Where that
+// makes more than 32, which no CTA holds, the two are added up before.  (The end is reduce_row's: as a function of both it moved registers in the launches
+// with two chunks a thread, fp32 3000 x 2304 9.6 -> 10.2 us.)
+template <bool SUM, bool MAX>
+__device__ __forceinline__ void reduce_row_twofold(float &s, float more, uint32_t &a, uint2 *part)
+{
+    uint32_t none = 0;
+    reduce_lanes<SUM, MAX>(s, a, 32);
+    reduce_lanes<SUM, false>(more, none, 32);
+    const int lane = threadIdx.x & 31, own = blockDim.x >> 5;
+    const bool apart = SUM && own <= 16;
+    if (SUM && !apart) s += more;
+    if (lane == 0) {
+        part[threadIdx.x >> 5] = make_uint2(__float_as_uint(s), a);
+        if (apart) part[(threadIdx.x >> 5) + own] = make_uint2(__float_as_uint(more), 0);
+    }
+    __syncthreads();
+    const int warps = apart ? 2 * own : own;
+    const int lanes = warps <= 4 ? 4 : warps <= 8 ? 8 : 32, mine = lane & (lanes - 1);
+    const uint2 v = mine < warps ? part[mine] : make_uint2(0, 0);
+    s = __uint_as_float(v.x);
+    a = v.y;
+    reduce_lanes<SUM, false>(s, a, lanes);
+    if (MAX) a = __reduce_max_sync(0xFFFFFFFFu, a);
+}
+
 // gamma of a chunk, n (> 0) elements from its first on.  It is aligned as good as always, whatever the rows are.
 template <int LAYOUT>
 __device__ __forceinline__ void load_gamma(const float *gamma, bool wide, int n, uint64_t (&g)[4])
@@ -96,13 +122,13 @@ __device__ __forceinline__ void load_gamma(const float *gamma, bool wide, int n,
 // y = rstd w are those of w, and sum and maximum are taken in one pass (two passes with a meeting each: 43 968 x 4096 bf16 172 us).
 template <class T, bool NORM, bool QUANT, int LAYOUT>
 struct Row {
-    float sum = 0.0f;
+    float sum = 0.0f, sum_more = 0.0f;                   // sum_more: of the second half of a thread's chunks, where it has two halves
     uint32_t top = 0;                                    // bits of the largest magnitude: NaN is the largest of all
     uint64_t factor = 0;                                 // rstd, or what turns values into codes
     bool finite = true;
 
     // Takes values into sum and maximum; with codes behind the norm, v turns into w.
-    __device__ __forceinline__ void take(uint64_t (&v)[4], const uint64_t (&g)[4])
+    __device__ __forceinline__ void take(uint64_t (&v)[4], const uint64_t (&g)[4], bool more = false)
     {
         if (NORM) {
             uint64_t s = 0;
@@ -110,7 +136,8 @@ struct Row {
             for (int i = 0; i < 4; ++i) s = ptx::f32x2_fma(v[i], v[i], s);
             float lo, hi;
             ptx::f32x2_unpack(s, lo, hi);
-            sum += lo + hi;
+            if (more) sum_more += lo + hi;
+            else sum += lo + hi;
         }
         if (QUANT) {
             float t = __uint_as_float(top);
@@ -182,6 +209,9 @@ __device__ __forceinline__ void async_wait(int pending)       // at most so many
 // Rows in registers: thread t of a row's threads (LANES of a warp, or (0) the CTA) has the chunks t, t + threads, .. (CHUNKS of them).  Its
 // threads take `turns` rows; while one is worked on, the next `depth` are on their way to shared memory, each warp fetching what it will
 // read itself, so that no warp waits for another but in the reduction.  gamma comes from L1 for every row.
+// A thread with four chunks stands for the threads t and t + threads of the `half` that a launch with two chunks a thread has (the first has its chunks
+// 0 and 2; the last warp may have no second to stand for) and adds up as they would: which of the two launches takes a row, which goes by the
+// number of rows, does not show in its results.
 template <class T, bool NORM, bool QUANT, int LANES, int LAYOUT, int CHUNKS>
 __global__ void __launch_bounds__(LANES ? SHORT_THREADS : MAX_THREADS, LANES ? (CHUNKS > 1 ? 3 : 4) : 1) rows_kernel(const __grid_constant__ Rows p, int turns, int depth)
 {
@@ -193,16 +223,18 @@ __global__ void __launch_bounds__(LANES ? SHORT_THREADS : MAX_THREADS, LANES ? (
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int t = LANES ? threadIdx.x % GROUP : threadIdx.x, threads = LANES ? GROUP : blockDim.x, lane = threadIdx.x % GROUP;
-    const bool residual = NORM && p.r;
+    const bool residual = NORM && CHUNKS < 4 && p.r;                         // (with one, by_length() takes two chunks)
     const uint32_t slot_bytes = residual ? 2 * TENSOR : TENSOR, mine = ptx::smem_addr(ring) + threadIdx.x / GROUP * depth * slot_bytes;
     const long long first = (long long)blockIdx.x * turns * step, left = (p.M - first + step - 1) / step, m0 = first + (LANES ? threadIdx.x / GROUP : 0);
     const int rows = left < turns ? (int)left : turns;                       // turns of this CTA
     const int mine_rows = (int)min((long long)rows, (p.M - m0 + step - 1) / step);       // in the last, a group may have no row
+    const int half = (p.K + 511) / 512 * 32, K_more = t + threads < half ? p.K : 0;      // (four chunks a thread only)
+    auto length = [&](int i) { return CHUNKS == 4 && (i & 1) ? K_more : p.K; };          // of the row, as chunk i sees it
     int at[CHUNKS], n[CHUNKS];                                               // a chunk's first element, elements from there on
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
-        at[i] = 8 * (t + i * threads);
-        n[i] = p.K - at[i];
+        at[i] = 8 * (CHUNKS < 4 ? t + i * threads : t + (i & 1) * threads + (i >> 1) * half);
+        n[i] = length(i) - at[i];
     }
     // rows of this thread's, one after the other: read, fetched ahead, written
     const T *x = static_cast<const T *>(p.x) + m0 * p.ldx, *r = static_cast<const T *>(p.r) + m0 * p.ldr, *x_ahead = x, *r_ahead = r;
@@ -216,8 +248,8 @@ __global__ void __launch_bounds__(LANES ? SHORT_THREADS : MAX_THREADS, LANES ? (
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
                 const int a = at[i] - 8 * lane;                              // the group's first
-                C::template fetch_async<GROUP>(slot + i * BLOCK, x_ahead + a, p.K - a, lane);
-                if (residual) C::template fetch_async<GROUP>(slot + TENSOR + i * BLOCK, r_ahead + a, p.K - a, lane);
+                C::template fetch_async<GROUP>(slot + i * BLOCK, x_ahead + a, length(i) - a, lane);
+                if (residual) C::template fetch_async<GROUP>(slot + TENSOR + i * BLOCK, r_ahead + a, length(i) - a, lane);
             }
             x_ahead += step * p.ldx;
             r_ahead += step * p.ldr;
@@ -265,9 +297,10 @@ __global__ void __launch_bounds__(LANES ? SHORT_THREADS : MAX_THREADS, LANES ? (
             if (NORM && p.h && here && n[i] > 0) store8(h + at[i], LAYOUT == REGULAR || (p.wide_h && n[i] >= 8), n[i], v[i]);
             uint64_t g[4];
             if (NORM && QUANT) gamma(i, g);
-            row.take(v[i], g);
+            row.take(v[i], g, CHUNKS == 4 && (i & 1));
         }
-        reduce_row<LANES, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
+        if constexpr (CHUNKS == 4) reduce_row_twofold<NORM, QUANT>(row.sum, row.sum_more, row.top, part[turn & 1]);
+        else reduce_row<LANES, NORM, QUANT>(row.sum, row.top, part[turn & 1]);
         row.end(p, here ? scale : nullptr);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
@@ -441,9 +474,11 @@ cudaError_t by_length(const Rows &p, cudaStream_t st)
     if (chunks <= 32) return launch_rows<T, NORM, QUANT, 32, LAYOUT, 1>(p, SHORT_THREADS, st);
     if (chunks <= 64) return launch_rows<T, NORM, QUANT, 32, LAYOUT, 2>(p, SHORT_THREADS, st);
     // Four chunks a thread, half the warps, where arithmetic shows beside the little that is read: every warp spends some 250 instructions
-    // a row on what does not depend on its chunks.  43 968 x 4096 bf16, us with two / four: norm and codes 121 / 110, quantizer 80 / 80;
-    // 10 992 x 4096 33 / 30 and 22.7 / 20.9; but with a residual 50 / 52, norm alone 32 / 32, one row 1.9 / 2.5.
-    if (QUANT && !p.r && p.M >= 4096 && chunks > 128 && chunks <= 4 * MAX_THREADS) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
+    // a row on what does not depend on its chunks.  43 968 x 4096 bf16, us with two / four: norm and codes 121 / 102, quantizer 80 / 80;
+    // 10 992 x 4096 33 / 29.5 and 22.7 / 20.9; but with a residual 50 / 52, norm alone 32 / 32, one row 1.9 / 2.5.  The sum of a norm is added up
+    // in the same order by both; so rows too long for two chunks always take four behind a norm (few rows by
+    // long_rows_kernel / four: 1 x 32 768 5.3 / 4.9, 500 x 32 768 18.9 / 17.2, 2000 x 32 768 81 / 61, fp32 3000 x 17 000 99 / 70).
+    if (QUANT && !p.r && chunks > 128 && chunks <= 4 * MAX_THREADS && (p.M >= 4096 || (NORM && chunks > 2 * MAX_THREADS))) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
     if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
     return launch(long_rows_kernel<T, NORM, QUANT, LAYOUT>, dim3(p.M), MAX_THREADS, 0, st, p);
 }
