@@ -124,10 +124,12 @@ cudaError_t launch(const QvggtLinear &p, cudaStream_t st)
                               static_cast<T *>(p.Y), p.ldy, p.M, p.N, p.K);
 }
 
+// Up to eight rows as linear_plan::choose() sends them; more where the tiles kernel, which would take them, does not count so far (N beyond some
+// tens of millions).
 template <class T>
 cudaError_t by_rows(const QvggtLinear &p, cudaStream_t st)
 {
-    return p.M <= 8 ? launch<T, 1>(p, st) : p.M <= 16 ? launch<T, 2>(p, st) : launch<T, 4>(p, st);
+    return p.M <= 8 ? launch<T, 1>(p, st) : launch<T, 4>(p, st);
 }
 
 }  // namespace

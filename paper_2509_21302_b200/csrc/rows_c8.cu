@@ -478,7 +478,8 @@ cudaError_t by_length(const Rows &p, cudaStream_t st)
     // 10 992 x 4096 33 / 29.5 and 22.7 / 20.9; but with a residual 50 / 52, norm alone 32 / 32, one row 1.9 / 2.5.  The sum of a norm is added up
     // in the same order by both; so rows too long for two chunks always take four behind a norm (few rows by
     // long_rows_kernel / four: 1 x 32 768 5.3 / 4.9, 500 x 32 768 18.9 / 17.2, 2000 x 32 768 81 / 61, fp32 3000 x 17 000 99 / 70).
-    if (QUANT && !p.r && chunks > 128 && chunks <= 4 * MAX_THREADS && (p.M >= 4096 || (NORM && chunks > 2 * MAX_THREADS))) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
+    if constexpr (QUANT)
+        if (!p.r && chunks > 128 && chunks <= 4 * MAX_THREADS && (p.M >= 4096 || (NORM && chunks > 2 * MAX_THREADS))) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 4>(p, (chunks + 127) / 128 * 32, st);
     if (chunks <= 2 * MAX_THREADS) return launch_rows<T, NORM, QUANT, 0, LAYOUT, 2>(p, (chunks + 63) / 64 * 32, st);
     return launch(long_rows_kernel<T, NORM, QUANT, LAYOUT>, dim3(p.M), MAX_THREADS, 0, st, p);
 }

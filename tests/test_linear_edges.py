@@ -7,10 +7,13 @@ import paper_2509_21302_b200 as q
 CSRC = os.path.join(os.path.dirname(q.__file__), "csrc")
 PROGRAM = r"""
 #include <cstdio>
+#include "gemm_c8_plan.cuh"
 #include "linear_plan.cuh"
 using namespace linear_plan;
 int main()
 {
+    Split beyond = {};      // the sizes of test_gpu_linear_wide.py: meant for the tiles kernel, beyond what it counts with
+    if (choose(40, 67200003, 17, 148, &beyond) != TILES || gemm_c8::can_plan(40, 67200003)) { std::printf("not beyond the tiles kernel\n"); return 1; }
     for (long long N = 1; N <= 2147483647LL; N += N == 600 ? 2147483647LL - 1200 : 1) {
         Split s = {};
         if (N > 600 && choose(8, (int)N, 1, 148, &s) != SPLIT) { std::printf("N %lld: another kernel\n", N); return 1; }
