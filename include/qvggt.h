@@ -268,8 +268,8 @@ int qvggt_gelu_rotate_smooth_quantize_c8(const qvggt_weights_t *w, const void *X
 int qvggt_gelu(const void *X_bf16, long long ldx, int M, int K, void *Y_bf16, void *cuda_stream);
 
 /*
- * The rotation-free 8-bit path: the paper's "naive" W8A8 arm (Tab. "efficiency", 8/8 naive) and any layer whose codes do not come
- * from a rotated handle -- RMS norms, other widths, weights quantized elsewhere.  Rows of any length K from 1 to 131056, rows of any
+ * The rotation-free 8-bit path: layers whose codes do not come from a rotated handle -- RMS norms, other widths, weights quantized elsewhere,
+ * the quantizers and products of the paper's "naive" W8A8 arm (Tab. "efficiency", 8/8 naive).  Rows of any length K from 1 to 131056, rows of any
  * leading dimension from K on; activations, residual, results and bias are of one of three types; all arithmetic is fp32.  A row's results do not
  * depend on M, on the other rows, or on how rows are aligned: they are bit for bit those of the same row in a call of its own.
  *
@@ -300,7 +300,8 @@ int qvggt_dequantize_c8(const signed char *Xq8, long long ldq, const float *a_sc
  * RMS norm with the residual's addition:
  *   h[k] = X[k] + residual[k] (X[k] without residual),  Y[k] = (h[k] * rstd) * gamma[k],  rstd = 1 / sqrt(sum(h * h) / K + eps)
  * The sum is kept in fp32 for the norm; H, if given, receives it rounded to the type.  The squares are summed in fp32: rows whose
- * sum of squares is beyond its range give 0 (NaN where an element is infinite).
+ * sum of squares is beyond its range give 0 (NaN where an element is infinite).  With eps = 0, rows whose sum is 0 in fp32 -- zeros, and values below
+ * some 1e-23 -- are not finite.
  *   residual  [M, K] or NULL;  H [M, K] or NULL;  gamma fp32 [K];  eps >= 0, finite
  * H and Y may each be X or residual itself (the same pointer and stride), not overlap them, or one another, in any other way.
  */
